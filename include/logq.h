@@ -20,6 +20,11 @@
  *                        inverse-Hessian factor, then W -> packed codes
  *   logq_linear          device: codes, codebook, X[B][K] -> Y[B][N] = X * What^T
  *   logq_linear_grouped  the same for up to four matrices sharing X, one launch
+ * and, between the linear layers of a decoder, its key/value cache in 4-bit
+ * Log_b codes:
+ *   logq_kv_plan         device: request lengths -> block tables, slot map, positions
+ *   logq_kv_append       device: 16-bit keys and values -> codes in their slots
+ *   logq_kv_attention    device: queries x the cached tokens of their requests
  *
  * Conventions shared by every call:
  *   - Matrices are row-major and contiguous.  W and What are [N][K]
@@ -351,6 +356,124 @@ logq_status logq_linear_grouped(const logq_linear_item* items, int count, const 
  * its launches.  A smaller workspace (at least logq_workspace_bytes()) is
  * accepted and only reduces the splits.  0 for invalid sizes. */
 size_t logq_linear_grouped_workspace_bytes(int64_t B, const int64_t* N, int count, int64_t K, int bits);
+
+/*
+ * Paged key/value cache in 4-bit Log_b codes.
+ *
+ * A page holds page_size tokens of every kv head; a slot is page * page_size +
+ * offset.  Each token's key (and value) vector of a kv head is stored as
+ *   codes: head_dim / 2 bytes, dimension 2j in the low and 2j + 1 in the high
+ *          half of byte j, c = sign << 3 | m as above (n = 4);
+ *   range: its largest magnitude, in the cache's 16-bit type (exact: it is one
+ *          of the vector's values).
+ * A code stands for range * level16[c], level16 = the codebook's table of the
+ * cache's type, the codebook (bits 4) built for range 1.  The code of x is
+ * Eq. (1) with the vector's range as w_max: m = #{ j < 7 : |x| >= thresh[j] *
+ * range }, the product rounded to fp32; a zero vector has range 0 and codes 0.
+ * A vector that holds NaN or Inf is stored with range NaN and codes 0, so every
+ * query that sees it answers NaN and no other query is touched.
+ * Layout: codes [pages][heads][page_size][head_dim / 2], ranges
+ * [pages][heads][page_size], contiguous.
+ */
+typedef struct logq_kv_cache {
+    uint8_t* k_codes;           /* device, 16-byte aligned (as all four) */
+    void* k_range;
+    uint8_t* v_codes;
+    void* v_range;
+    const logq_codebook* k_cb;  /* host: codebooks with bits 4 and range 1 */
+    const logq_codebook* v_cb;
+    int64_t pages;              /* 1 .. 2^31 - 1 */
+    int32_t page_size;          /* a power of two, 16 .. 1024 */
+    int32_t heads;              /* kv heads, 1 .. 1024 */
+    int32_t head_dim;           /* 64 or 128 */
+    int32_t dtype;              /* LOGQ_BF16 or LOGQ_F16: keys, values, queries, ranges */
+} logq_kv_cache;
+
+/* Bytes of k_codes (and of v_codes) for a cache of that size; the ranges take
+ * 4 / head_dim times as much.  0 for invalid sizes. */
+size_t logq_kv_code_bytes(int64_t pages, int32_t page_size, int32_t heads, int32_t head_dim);
+
+/*
+ * One step's bookkeeping for `requests` requests, from their lengths alone:
+ * where each new token goes and which pages that takes.  Device memory:
+ *   ctx_len[requests]    tokens request r has in the cache
+ *   new_len[requests]    tokens it adds in this step (0 allowed); a negative
+ *                        value says that the request has ended
+ *   block_table[requests][table_width]  page of request r's tokens
+ *                        i * page_size .. : the first ceil(ctx_len / page_size)
+ *                        entries are read, those this step adds are written
+ *   ring[ring_size], ring_state = { head, count }  the free pages: ring[(head +
+ *                        i) mod ring_size], i < count.  New pages are taken from
+ *                        the head in request order; the pages of ended requests
+ *                        are put behind the tail (in request and page order) and
+ *                        are free from the next step on.  ring_size = the pages
+ *                        of the cache always suffices.
+ * Outputs:
+ *   q_start[requests + 1]  exclusive sum of max(new_len, 0), at most max_tokens
+ *   kv_len[requests]     ctx_len + new_len; 0 for a request that ended or is refused
+ *   positions[max_tokens], slots[max_tokens]  of token q_start[r] + i: ctx_len[r] +
+ *                        i and its slot; both -1 for tokens of refused requests
+ *                        and for the entries from q_start[requests] on
+ *   ring_state_out[2]    the ring's new head and count; may be ring_state itself
+ * A request is refused (it keeps its pages and takes none, its tokens have no
+ * slot, its queries see no key) when its tokens end beyond max_tokens, its pages
+ * do not fit table_width, its length is negative, or it needs pages and those of
+ * the requests up to it are more than `count`.  Nothing else may overlap.
+ * workspace: as logq_quantize's; needed only when ring_state_out == ring_state
+ * (NULL is then refused).  Asynchronous.  Errors: LOGQ_ERR_INVALID_ARG,
+ * LOGQ_ERR_WORKSPACE, LOGQ_ERR_CUDA. */
+logq_status logq_kv_plan(const int32_t* ctx_len, const int32_t* new_len, int64_t requests, int32_t* block_table,
+                         int64_t table_width, int32_t page_size, int32_t* ring, int64_t ring_size,
+                         const int32_t* ring_state, int32_t* ring_state_out, int64_t max_tokens, int32_t* q_start,
+                         int32_t* kv_len, int32_t* positions, int64_t* slots, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * Quantise `tokens` keys and values into the cache.  k, v (device, the cache's
+ * type): [tokens][heads][head_dim] with k_stride / v_stride elements from token
+ * to token (a multiple of 8, at least heads * head_dim: slices of a fused
+ * projection serve), 16-byte aligned.  slots (device, int64[tokens]): a token
+ * whose slot is negative or beyond the cache is not stored.  Two tokens of a
+ * call must not share a slot.  k_values, v_values (device, [tokens][heads]
+ * [head_dim] contiguous, 16-byte aligned, both or neither NULL) receive what the
+ * codes stand for, range * level16 rounded to the type (NaN for a vector with
+ * NaN or Inf), for every token.  tokens = 0 does nothing.  Asynchronous.
+ * Errors: LOGQ_ERR_INVALID_ARG, LOGQ_ERR_UNSUPPORTED (head_dim, type, code
+ * width), LOGQ_ERR_CUDA. */
+logq_status logq_kv_append(const logq_kv_cache* cache, const void* k, int64_t k_stride, const void* v,
+                           int64_t v_stride, const int64_t* slots, int64_t tokens, void* k_values, void* v_values,
+                           void* stream);
+
+/* Workspace of logq_kv_attention on the current device for these heads: partial
+ * results of key ranges that several CTAs share.  Zero-filled once by the caller,
+ * 256-byte aligned; calls that share it must be ordered on one stream.  0 for
+ * invalid sizes. */
+size_t logq_kv_attention_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+
+/*
+ * Attention of `tokens` queries over the cached tokens of their requests (the
+ * step's own tokens appended before).  q (device, the cache's type):
+ * [tokens][q_heads][head_dim] with q_stride elements from token to token (a
+ * multiple of 8); out: the same type, [tokens][q_heads][head_dim] contiguous;
+ * both 16-byte aligned.  q_heads is a multiple of cache->heads; query head z
+ * reads kv head z / (q_heads / heads).
+ *   Token q_start[r] + i of request r (q_start, kv_len, block_table as
+ *   logq_kv_plan gives them; device) sits at position p = kv_len[r] -
+ *   (q_start[r + 1] - q_start[r]) + i and sees the keys max(0, p - window + 1)
+ *   .. p (window = 0: 0 .. p) that lie below kv_len[r] and table_width *
+ *   page_size and in pages the cache has:
+ *   out = sum_j softmax_j(scale * q . k_j) v_j.  A token that sees no key
+ *   (p < 0, kv_len 0) gives zeros.  Tokens outside every request are not written.
+ *   max_q: an upper bound of a request's tokens in this call; it only chooses
+ *   kernels (any value gives the same results up to rounding).
+ * Scores, softmax and sums are fp32; the weights that multiply the values are
+ * rounded to fp16 (scaled by the value's range, so that none overflows).
+ * Asynchronous.  Errors: LOGQ_ERR_INVALID_ARG, LOGQ_ERR_UNSUPPORTED,
+ * LOGQ_ERR_WORKSPACE, LOGQ_ERR_CUDA. */
+logq_status logq_kv_attention(const logq_kv_cache* cache, const void* q, int64_t q_stride, int32_t q_heads,
+                              int64_t tokens, const int32_t* q_start, const int32_t* kv_len, int64_t requests,
+                              const int32_t* block_table, int64_t table_width, double scale, int64_t window,
+                              int64_t max_q, void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Synchronise `stream`, read the device error word of `workspace`, clear it,
  * and return LOGQ_OK or LOGQ_ERR_TIMEOUT.  *detail (host, may be NULL)

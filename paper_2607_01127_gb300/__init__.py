@@ -11,6 +11,9 @@ The functions carry the C names:
   logq_quantize(W, bits, base, range, flags, ...)       -> (codes, Codebook)
   logq_linear(codes, cb, X, N, K, y_dtype, ...)         -> Y
   logq_workspace_status(workspace)                      -> (status, detail)
+  logq_kv_plan(ctx_len, new_len, block_table, ...)      -> (q_start, kv_len, positions, slots, ring_state)
+  logq_kv_append(cache, k, v, slots)                    -> None, or the stored values
+  logq_kv_attention(cache, q, q_start, kv_len, block_table, ...) -> out
   logq_status_string(status), logq_device_sm_count()
 
 There is no CPU fallback: the first call raises ImportError when the library
@@ -42,7 +45,8 @@ EXPORTED = ("logq_build_codebook", "logq_packed_bytes", "logq_workspace_bytes", 
             "logq_linear", "logq_workspace_status", "logq_status_string", "logq_device_sm_count",
             "logq_quantize_noalloc", "logq_linear_grouped", "logq_energy_scratch_bytes",
             "logq_quantize_energy", "logq_gptq_factor_scratch_bytes", "logq_gptq_factor",
-            "logq_gptq_scratch_bytes", "logq_gptq")
+            "logq_gptq_scratch_bytes", "logq_gptq", "logq_kv_code_bytes", "logq_kv_plan", "logq_kv_append",
+            "logq_kv_attention_workspace_bytes", "logq_kv_attention")
 
 
 class Codebook(ctypes.Structure):
@@ -69,6 +73,23 @@ class LinearItem(ctypes.Structure):
         ("cb", ctypes.POINTER(Codebook)),
         ("N", ctypes.c_int64),
         ("Y", ctypes.c_void_p),
+    ]
+
+
+class KVCacheStruct(ctypes.Structure):
+    """Mirror of ``logq_kv_cache`` (include/logq.h)."""
+    _fields_ = [
+        ("k_codes", ctypes.c_void_p),
+        ("k_range", ctypes.c_void_p),
+        ("v_codes", ctypes.c_void_p),
+        ("v_range", ctypes.c_void_p),
+        ("k_cb", ctypes.POINTER(Codebook)),
+        ("v_cb", ctypes.POINTER(Codebook)),
+        ("pages", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
     ]
 
 
@@ -120,6 +141,18 @@ def _load() -> ctypes.CDLL:
     lib.logq_linear_grouped.restype = c_int
     lib.logq_workspace_status.argtypes = [P, P, ctypes.POINTER(ctypes.c_uint32)]
     lib.logq_workspace_status.restype = c_int
+    c_i32, c_sz = ctypes.c_int32, ctypes.c_size_t
+    lib.logq_kv_code_bytes.argtypes = [c_i64, c_i32, c_i32, c_i32]
+    lib.logq_kv_code_bytes.restype = c_sz
+    lib.logq_kv_plan.argtypes = [P, P, c_i64, P, c_i64, c_i32, P, c_i64, P, P, c_i64, P, P, P, P, P, c_sz, P]
+    lib.logq_kv_plan.restype = c_int
+    lib.logq_kv_append.argtypes = [ctypes.POINTER(KVCacheStruct), P, c_i64, P, c_i64, P, c_i64, P, P, P]
+    lib.logq_kv_append.restype = c_int
+    lib.logq_kv_attention_workspace_bytes.argtypes = [c_i32, c_i32, c_i32]
+    lib.logq_kv_attention_workspace_bytes.restype = c_sz
+    lib.logq_kv_attention.argtypes = [ctypes.POINTER(KVCacheStruct), P, c_i64, c_i32, c_i64, P, P, c_i64, P, c_i64,
+                                      c_dbl, c_i64, c_i64, P, P, c_sz, P]
+    lib.logq_kv_attention.restype = c_int
     lib.logq_status_string.argtypes = [c_int]
     lib.logq_status_string.restype = ctypes.c_char_p
     lib.logq_device_sm_count.argtypes = []
@@ -378,3 +411,145 @@ def logq_workspace_status(workspace, stream=None):
 
 def logq_device_sm_count() -> int:
     return int(_lib().logq_device_sm_count())
+
+
+# ------------------------------------------------ paged 4-bit key/value cache ---
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream_int(stream, device):
+    import torch
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+class KVCache:
+    """A paged key/value cache in 4-bit Log_b codes (``logq_kv_cache``) over its tensors:
+    k_codes, v_codes uint8 [pages, heads, page_size, head_dim / 2], k_range, v_range
+    [pages, heads, page_size] in bf16 or fp16, and two 4-bit codebooks of range 1."""
+
+    def __init__(self, k_codes, k_range, v_codes, v_range, k_cb: Codebook, v_cb: Codebook):
+        import torch
+        assert k_codes.dim() == 4 and k_codes.dtype == torch.uint8 and k_codes.is_cuda
+        pages, heads, page_size, half = k_codes.shape
+        assert v_codes.shape == k_codes.shape and v_codes.dtype == torch.uint8
+        assert k_range.shape == k_codes.shape[:3] and v_range.shape == k_codes.shape[:3]
+        assert k_range.dtype == v_range.dtype and k_range.dtype in (torch.bfloat16, torch.float16)
+        for x in (k_codes, k_range, v_codes, v_range):
+            assert x.is_contiguous() and x.device == k_codes.device, "the cache's tensors are contiguous, on one device"
+        self.k_codes, self.k_range, self.v_codes, self.v_range = k_codes, k_range, v_codes, v_range
+        self.k_cb, self.v_cb = k_cb, v_cb
+        self.pages, self.heads, self.page_size, self.head_dim = pages, heads, page_size, 2 * half
+        self.dtype, self.device = k_range.dtype, k_codes.device
+        self._struct = KVCacheStruct(k_codes.data_ptr(), k_range.data_ptr(), v_codes.data_ptr(), v_range.data_ptr(),
+                                     ctypes.pointer(k_cb), ctypes.pointer(v_cb), pages, page_size, heads, 2 * half,
+                                     _dtype_code(k_range.dtype))
+        self._ref = ctypes.byref(self._struct)
+
+
+def new_kv_cache(pages: int, page_size: int, heads: int, head_dim: int, dtype=None, base: float = 1.5,
+                 v_base: float | None = None, device=None) -> KVCache:
+    """An empty cache whose codebooks have these bases (v_base: base when not given)."""
+    import torch
+    n = int(_lib().logq_kv_code_bytes(int(pages), int(page_size), int(heads), int(head_dim)))
+    if n == 0:
+        raise LogqError(LOGQ_ERR_INVALID_ARG, "new_kv_cache")
+    dev = device or "cuda"
+    shape = (pages, heads, page_size)
+    codes = [torch.zeros(*shape, head_dim // 2, dtype=torch.uint8, device=dev) for _ in range(2)]
+    ranges = [torch.zeros(*shape, dtype=dtype or torch.bfloat16, device=dev) for _ in range(2)]
+    return KVCache(codes[0], ranges[0], codes[1], ranges[1], logq_build_codebook(4, base, 1.0),
+                   logq_build_codebook(4, base if v_base is None else v_base, 1.0))
+
+
+def logq_kv_attention_workspace_bytes(q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(_lib().logq_kv_attention_workspace_bytes(int(q_heads), int(kv_heads), int(head_dim)))
+
+
+def new_kv_workspace(q_heads: int, kv_heads: int, head_dim: int, device=None):
+    """Zero-filled workspace of logq_kv_attention (calls on one stream may share it)."""
+    import torch
+    n = logq_kv_attention_workspace_bytes(q_heads, kv_heads, head_dim)
+    if n == 0:
+        raise LogqError(LOGQ_ERR_INVALID_ARG, "new_kv_workspace")
+    return torch.zeros(n, dtype=torch.uint8, device=device or "cuda")
+
+
+def logq_kv_plan(ctx_len, new_len, block_table, ring, ring_state, page_size: int, max_tokens: int,
+                 inplace: bool = True, workspace=None, stream=None):
+    """One step's bookkeeping: takes pages from the ring into block_table (int32 [requests, width]) and
+    returns (q_start, kv_len, positions, slots, ring_state).  ring_state is updated in place (with a
+    workspace of logq_workspace_bytes(), new when none is given), or left as it was with inplace=False."""
+    import torch
+    i32, dev = torch.int32, ctx_len.device
+    for x in (ctx_len, new_len, block_table, ring, ring_state):
+        assert x.dtype == i32 and x.is_contiguous() and x.device == dev and x.is_cuda, "int32 device tensors expected"
+    n = ctx_len.numel()
+    assert new_len.numel() == n and block_table.dim() == 2 and block_table.shape[0] == n and ring_state.numel() == 2
+    ints = torch.empty(2 * n + 3 + max_tokens, dtype=i32, device=dev)
+    q_start, kv_len, out, positions = ints.split([n + 1, n, 2, max_tokens])
+    slots = torch.empty(max_tokens, dtype=torch.int64, device=dev)
+    if inplace:
+        out = ring_state
+        if workspace is None:
+            workspace = new_workspace(dev)
+    st = _lib().logq_kv_plan(ctx_len.data_ptr(), new_len.data_ptr(), n, block_table.data_ptr(), block_table.shape[1],
+                             page_size, ring.data_ptr(), ring.numel(), ring_state.data_ptr(), out.data_ptr(),
+                             max_tokens, q_start.data_ptr(), kv_len.data_ptr(), positions.data_ptr(),
+                             slots.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                             _stream_int(stream, dev))
+    _check(st, "logq_kv_plan")
+    return q_start, kv_len, positions, slots, out
+
+
+def _rows(x, heads, dim, cache, what):
+    """Element stride between the tokens of x [tokens, heads, dim] whose heads are contiguous."""
+    assert x.dim() == 3 and x.shape[1] == heads and x.shape[2] == dim and x.dtype == cache.dtype, \
+        f"{what} must be [tokens, {heads}, {dim}] in the cache's dtype"
+    assert x.device == cache.device and x.stride(2) == 1 and x.stride(1) == dim, f"the heads of {what} must be contiguous"
+    return x.stride(0) if x.shape[0] > 1 else heads * dim
+
+
+def logq_kv_append(cache: KVCache, k, v, slots, values: bool = False, stream=None):
+    """Quantise keys and values [tokens, heads, head_dim] (token stride free) into the slots (int64).
+    values=True returns (k_values, v_values): what the stored codes stand for."""
+    import torch
+    ks, vs = _rows(k, cache.heads, cache.head_dim, cache, "k"), _rows(v, cache.heads, cache.head_dim, cache, "v")
+    n = k.shape[0]
+    assert v.shape[0] == n and slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() >= n
+    assert slots.device == cache.device
+    kv = vv = None
+    if values:
+        kv, vv = torch.empty(2, n, cache.heads, cache.head_dim, dtype=cache.dtype, device=cache.device).unbind(0)
+    st = _lib().logq_kv_append(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), n, _ptr(kv), _ptr(vv),
+                               _stream_int(stream, cache.device))
+    _check(st, "logq_kv_append")
+    return (kv, vv) if values else None
+
+
+def logq_kv_attention(cache: KVCache, q, q_start, kv_len, block_table, scale: float | None = None, window: int = 0,
+                      max_q: int | None = None, out=None, workspace=None, stream=None):
+    """Causal attention of q [tokens, q_heads, head_dim] (token stride free) over the cached tokens of
+    its requests; scale defaults to head_dim ** -0.5, max_q (a bound of a request's tokens, for the
+    choice of kernels) to tokens.  Returns out [tokens, q_heads, head_dim]."""
+    import torch
+    tokens, hq = q.shape[0], q.shape[1]
+    qs = _rows(q, hq, cache.head_dim, cache, "q")
+    n = kv_len.numel()
+    for x in (q_start, kv_len, block_table):
+        assert x.dtype == torch.int32 and x.is_contiguous() and x.device == cache.device, "int32 device tensors expected"
+    assert q_start.numel() == n + 1 and block_table.dim() == 2 and block_table.shape[0] == n
+    if out is None:
+        out = torch.empty(tokens, hq, cache.head_dim, dtype=q.dtype, device=q.device)
+    else:
+        assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous() and out.device == q.device
+    if workspace is None:
+        workspace = new_kv_workspace(hq, cache.heads, cache.head_dim, cache.device)
+    st = _lib().logq_kv_attention(cache._ref, q.data_ptr(), qs, hq, tokens, q_start.data_ptr(), kv_len.data_ptr(), n,
+                                  block_table.data_ptr(), block_table.shape[1],
+                                  cache.head_dim ** -0.5 if scale is None else scale, window,
+                                  tokens if max_q is None else max_q, out.data_ptr(), workspace.data_ptr(),
+                                  workspace.numel(), _stream_int(stream, cache.device))
+    _check(st, "logq_kv_attention")
+    return out

@@ -14,7 +14,8 @@ struct Workspace {
     uint32_t nonfinite;     // 1 when a NaN / Inf weight was seen
     uint32_t error;         // device error word: LOGQ_ERR_TIMEOUT when a wait gave up
     uint32_t detail;        // which wait gave up (implementation code)
-    uint32_t reserved[60];
+    uint32_t reserved[59];
+    uint32_t ticket;        // arrivals of logq_kv_plan's CTAs (0 between calls)
 };
 static_assert(sizeof(Workspace) == 256, "workspace layout");
 constexpr size_t kWorkspaceBytes = sizeof(Workspace);

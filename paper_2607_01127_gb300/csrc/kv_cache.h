@@ -1,0 +1,77 @@
+// Kernel parameters of the paged 4-bit key/value cache, after validation.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "internal.h"
+
+namespace logq {
+
+struct KvPlanParams {
+    const int32_t* ctx_len;
+    const int32_t* new_len;
+    int64_t requests;
+    int32_t* block_table;
+    int64_t table_width;
+    int32_t page_size, page_shift;
+    int32_t* ring;
+    int64_t ring_size;
+    const int32_t* ring_state;
+    int32_t* ring_state_out;
+    int64_t max_tokens;
+    int32_t* q_start;
+    int32_t* kv_len;
+    int32_t* positions;
+    int64_t* slots;
+    Workspace* ws;           // in-place ring state: holds the arrival ticket; else null
+};
+
+struct KvAppendParams {
+    const uint16_t* k;
+    const uint16_t* v;
+    int64_t k_stride, v_stride;
+    const int64_t* slots;
+    int64_t tokens;
+    uint16_t* k_values;      // null: values are not wanted
+    uint16_t* v_values;
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    uint16_t* k_range;
+    uint16_t* v_range;
+    int64_t pages;
+    int32_t page_size, page_shift, heads, pad_;
+    float thresh[2][7];      // k, v: decision boundaries for range 1
+    uint16_t lvl16[2][16];   // k, v: levels in the cache's type
+};
+
+struct KvAttendParams {
+    const uint8_t* k_codes;
+    const uint8_t* v_codes;
+    const uint16_t* k_range;
+    const uint16_t* v_range;
+    int64_t pages;
+    int32_t page_size, page_shift, heads, group;     // group: query heads per kv head
+    const uint16_t* q;
+    int64_t q_stride;
+    int64_t tokens;
+    const int32_t* q_start;
+    const int32_t* kv_len;
+    int64_t requests;
+    const int32_t* block_table;
+    int64_t table_width;
+    float scale_log2;        // scale * log2(e): the softmax runs in base 2
+    int32_t pad_;
+    int64_t window;          // 0: none
+    uint16_t* out;
+    Workspace* ws;
+    uint16_t k_lvl[16];      // in the cache's type
+    uint16_t v_lvl[16];      // in fp16, whatever the cache's type
+};
+
+cudaError_t launch_kv_plan(const KvPlanParams& p, cudaStream_t s);
+cudaError_t launch_kv_append(const KvAppendParams& p, int head_dim, bool f16, cudaStream_t s);
+size_t kv_attention_workspace_bytes(int head_dim);
+cudaError_t launch_kv_attention(const KvAttendParams& p, int head_dim, bool f16, int64_t max_q, cudaStream_t s);
+
+}  // namespace logq

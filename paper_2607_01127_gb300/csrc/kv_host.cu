@@ -1,0 +1,215 @@
+// C-ABI front of the paged 4-bit key/value cache: argument validation and
+// dispatch (logq_kv_*).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+#include <string.h>
+
+#include "internal.h"
+#include "kv_cache.h"
+
+using namespace logq;
+
+namespace {
+
+bool aligned(const void* p, uintptr_t a) { return p && (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+bool valid_page_size(int32_t n) { return n >= 16 && n <= 1024 && (n & (n - 1)) == 0; }
+
+int log2_of(int32_t n)
+{
+    int s = 0;
+    while ((1 << s) < n) ++s;
+    return s;
+}
+
+bool supported_dim(int32_t d) { return d == 64 || d == 128; }
+
+logq_status check_cache(const logq_kv_cache* c)
+{
+    if (!c || !aligned(c->k_codes, 16) || !aligned(c->k_range, 16) || !aligned(c->v_codes, 16) ||
+        !aligned(c->v_range, 16) || !c->k_cb || !c->v_cb)
+        return LOGQ_ERR_INVALID_ARG;
+    if (c->pages < 1 || c->pages > 0x7fffffffll || !valid_page_size(c->page_size) || c->heads < 1 || c->heads > 1024)
+        return LOGQ_ERR_INVALID_ARG;
+    if (c->head_dim < 1) return LOGQ_ERR_INVALID_ARG;
+    if (!supported_dim(c->head_dim) || (c->dtype != LOGQ_BF16 && c->dtype != LOGQ_F16)) return LOGQ_ERR_UNSUPPORTED;
+    for (const logq_codebook* cb : {c->k_cb, c->v_cb}) {
+        if (cb->bits != 4) return LOGQ_ERR_UNSUPPORTED;
+        if (cb->qmax != 7 || cb->range != 1.0) return LOGQ_ERR_INVALID_ARG;
+    }
+    return LOGQ_OK;
+}
+
+uint16_t f16_of_bf16(uint16_t b)
+{
+    __nv_bfloat16 x;
+    memcpy(&x, &b, 2);
+    const __half h = __float2half_rn(__bfloat162float(x));
+    uint16_t r;
+    memcpy(&r, &h, 2);
+    return r;
+}
+
+logq_status status_of(cudaError_t e)
+{
+    if (e == cudaErrorNotSupported) return LOGQ_ERR_UNSUPPORTED;
+    return e == cudaSuccess ? LOGQ_OK : LOGQ_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t logq_kv_code_bytes(int64_t pages, int32_t page_size, int32_t heads, int32_t head_dim)
+{
+    if (pages < 1 || pages > 0x7fffffffll || !valid_page_size(page_size) || heads < 1 || heads > 1024 ||
+        !supported_dim(head_dim))
+        return 0;
+    return (size_t)pages * (size_t)page_size * (size_t)heads * (size_t)(head_dim / 2);
+}
+
+logq_status logq_kv_plan(const int32_t* ctx_len, const int32_t* new_len, int64_t requests, int32_t* block_table,
+                         int64_t table_width, int32_t page_size, int32_t* ring, int64_t ring_size,
+                         const int32_t* ring_state, int32_t* ring_state_out, int64_t max_tokens, int32_t* q_start,
+                         int32_t* kv_len, int32_t* positions, int64_t* slots, void* workspace,
+                         size_t workspace_bytes, void* stream)
+{
+    if (requests < 0 || requests > 0x7ffffffell || max_tokens < 0 || max_tokens > 0x7fffffffll ||
+        !valid_page_size(page_size) || table_width < 1 || table_width > 0x7fffffffll || ring_size < 1 ||
+        ring_size > 0x7fffffffll)
+        return LOGQ_ERR_INVALID_ARG;
+    if (requests > 0 && (!aligned(ctx_len, 4) || !aligned(new_len, 4) || !aligned(block_table, 4) || !aligned(kv_len, 4)))
+        return LOGQ_ERR_INVALID_ARG;
+    if (max_tokens > 0 && (!aligned(positions, 4) || !aligned(slots, 8))) return LOGQ_ERR_INVALID_ARG;
+    if (!aligned(ring, 4) || !aligned(ring_state, 4) || !aligned(ring_state_out, 4) || !aligned(q_start, 4))
+        return LOGQ_ERR_INVALID_ARG;
+    const bool in_place = ring_state == ring_state_out;
+    if (in_place && (!aligned(workspace, 16) || workspace_bytes < kWorkspaceBytes)) return LOGQ_ERR_WORKSPACE;
+
+    KvPlanParams p;
+    memset(&p, 0, sizeof p);
+    p.ctx_len = ctx_len;
+    p.new_len = new_len;
+    p.requests = requests;
+    p.block_table = block_table;
+    p.table_width = table_width;
+    p.page_size = page_size;
+    p.page_shift = log2_of(page_size);
+    p.ring = ring;
+    p.ring_size = ring_size;
+    p.ring_state = ring_state;
+    p.ring_state_out = ring_state_out;
+    p.max_tokens = max_tokens;
+    p.q_start = q_start;
+    p.kv_len = kv_len;
+    p.positions = positions;
+    p.slots = slots;
+    p.ws = in_place ? static_cast<Workspace*>(workspace) : nullptr;
+    return status_of(launch_kv_plan(p, static_cast<cudaStream_t>(stream)));
+}
+
+logq_status logq_kv_append(const logq_kv_cache* cache, const void* k, int64_t k_stride, const void* v,
+                           int64_t v_stride, const int64_t* slots, int64_t tokens, void* k_values, void* v_values,
+                           void* stream)
+{
+    const logq_status st = check_cache(cache);
+    if (st != LOGQ_OK) return st;
+    const int64_t row = (int64_t)cache->heads * cache->head_dim;
+    if (tokens < 0 || tokens > 0x7fffffffll || k_stride < row || v_stride < row || (k_stride & 7) || (v_stride & 7) ||
+        k_stride > (int64_t(1) << 31) || v_stride > (int64_t(1) << 31))
+        return LOGQ_ERR_INVALID_ARG;
+    if ((k_values == nullptr) != (v_values == nullptr)) return LOGQ_ERR_INVALID_ARG;
+    if (k_values && (!aligned(k_values, 16) || !aligned(v_values, 16))) return LOGQ_ERR_INVALID_ARG;
+    if (tokens == 0) return LOGQ_OK;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return LOGQ_ERR_INVALID_ARG;
+
+    const bool f16 = cache->dtype == LOGQ_F16;
+    KvAppendParams p;
+    memset(&p, 0, sizeof p);
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.k_stride = k_stride;
+    p.v_stride = v_stride;
+    p.slots = slots;
+    p.tokens = tokens;
+    p.k_values = static_cast<uint16_t*>(k_values);
+    p.v_values = static_cast<uint16_t*>(v_values);
+    p.k_codes = cache->k_codes;
+    p.v_codes = cache->v_codes;
+    p.k_range = static_cast<uint16_t*>(cache->k_range);
+    p.v_range = static_cast<uint16_t*>(cache->v_range);
+    p.pages = cache->pages;
+    p.page_size = cache->page_size;
+    p.page_shift = log2_of(cache->page_size);
+    p.heads = cache->heads;
+    for (int i = 0; i < 2; ++i) {
+        const logq_codebook* cb = i ? cache->v_cb : cache->k_cb;
+        memcpy(p.thresh[i], cb->thresh, sizeof p.thresh[i]);
+        memcpy(p.lvl16[i], f16 ? cb->level_f16 : cb->level_bf16, sizeof p.lvl16[i]);
+    }
+    return status_of(launch_kv_append(p, cache->head_dim, f16, static_cast<cudaStream_t>(stream)));
+}
+
+size_t logq_kv_attention_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim)
+{
+    if (kv_heads < 1 || kv_heads > 1024 || q_heads < kv_heads || q_heads > 65536 || q_heads % kv_heads ||
+        !supported_dim(head_dim))
+        return 0;
+    return kv_attention_workspace_bytes(head_dim);
+}
+
+logq_status logq_kv_attention(const logq_kv_cache* cache, const void* q, int64_t q_stride, int32_t q_heads,
+                              int64_t tokens, const int32_t* q_start, const int32_t* kv_len, int64_t requests,
+                              const int32_t* block_table, int64_t table_width, double scale, int64_t window,
+                              int64_t max_q, void* out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const logq_status st = check_cache(cache);
+    if (st != LOGQ_OK) return st;
+    if (q_heads < 1 || q_heads > 65536 || q_heads % cache->heads) return LOGQ_ERR_INVALID_ARG;
+    if (tokens < 0 || tokens > 0x7fffffffll / q_heads || requests < 0 || requests > 0x7ffffffell || max_q < 0 ||
+        window < 0 || !isfinite(scale))
+        return LOGQ_ERR_INVALID_ARG;
+    if (table_width < 1 || table_width > 0x7fffffffll / cache->page_size) return LOGQ_ERR_INVALID_ARG;
+    if (q_stride < (int64_t)q_heads * cache->head_dim || (q_stride & 7) || q_stride > (int64_t(1) << 31))
+        return LOGQ_ERR_INVALID_ARG;
+    if (!aligned(workspace, 256) ||
+        workspace_bytes < logq_kv_attention_workspace_bytes(q_heads, cache->heads, cache->head_dim))
+        return LOGQ_ERR_WORKSPACE;
+    if (tokens == 0 || requests == 0) return LOGQ_OK;
+    if (!aligned(q, 16) || !aligned(out, 16) || !aligned(q_start, 4) || !aligned(kv_len, 4) || !aligned(block_table, 4))
+        return LOGQ_ERR_INVALID_ARG;
+
+    const bool f16 = cache->dtype == LOGQ_F16;
+    KvAttendParams p;
+    memset(&p, 0, sizeof p);
+    p.k_codes = cache->k_codes;
+    p.v_codes = cache->v_codes;
+    p.k_range = static_cast<const uint16_t*>(cache->k_range);
+    p.v_range = static_cast<const uint16_t*>(cache->v_range);
+    p.pages = cache->pages;
+    p.page_size = cache->page_size;
+    p.page_shift = log2_of(cache->page_size);
+    p.heads = cache->heads;
+    p.group = q_heads / cache->heads;
+    p.q = static_cast<const uint16_t*>(q);
+    p.q_stride = q_stride;
+    p.tokens = tokens;
+    p.q_start = q_start;
+    p.kv_len = kv_len;
+    p.requests = requests;
+    p.block_table = block_table;
+    p.table_width = table_width;
+    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    p.window = window;
+    p.out = static_cast<uint16_t*>(out);
+    p.ws = static_cast<Workspace*>(workspace);
+    for (int c = 0; c < 16; ++c) {
+        p.k_lvl[c] = f16 ? cache->k_cb->level_f16[c] : cache->k_cb->level_bf16[c];
+        p.v_lvl[c] = f16 ? cache->v_cb->level_f16[c] : f16_of_bf16(cache->v_cb->level_bf16[c]);
+    }
+    return status_of(launch_kv_attention(p, cache->head_dim, f16, max_q < tokens ? max_q : tokens,
+                                         static_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"
