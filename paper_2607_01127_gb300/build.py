@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "liblogq.so")
 SOURCES = ["logq_host.cu", "quantize.cu", "energy.cu", "gptq.cu", "gemv.cu", "prefill.cu", "noalloc.cu",
-           "kv_cache.cu", "kv_attention.cu", "kv_host.cu"]
+           "kv_cache.cu", "kv_attention.cu", "kv_tiles.cu", "kv_host.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -39,6 +39,8 @@
 
 #include "internal.h"
 #include "kv_cache.h"
+#include "kv_device.h"
+#include "ptx.h"
 
 namespace logq {
 namespace {
@@ -46,25 +48,8 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStep = 16;                    // keys per warp step
-constexpr int kMaxCols = 16;                 // query rows per segment
 constexpr int kMinChunk = kWarps;            // steps per CTA, at least
-constexpr int kMaxCtasPerSm = 2;
-constexpr uint32_t kTabOff = 1024;           // shared address of dynamic shared memory (after the reserved area)
 constexpr uint32_t kTabBytes = 256 * 256;
-constexpr float kRefInit = -3.0e38f;
-constexpr float kRaise = 8.0f;               // log2 headroom before the reference is raised
-
-// Workspace: record | arrival counters [max CTAs] | partial results, two slots per CTA
-constexpr int kMaxCtas = 1024;
-constexpr size_t kCounterBytes = kMaxCtas * sizeof(uint32_t);
-__host__ __device__ constexpr size_t slot_floats(int d) { return (size_t)kMaxCols * (d + 2); }
-
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
-{
-    uint32_t r;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
-    return r;
-}
 
 template <uint32_t OFF>
 __device__ __forceinline__ uint32_t lds_tab(uint32_t off)
@@ -96,32 +81,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v)
     return r;
 }
 
-__device__ __forceinline__ float exp2_approx(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-template <bool F16>
-__device__ __forceinline__ float to_float(uint32_t b)
-{
-    if constexpr (F16) return __half2float(__ushort_as_half((unsigned short)b));
-    else return __uint_as_float(b << 16);
-}
-
-template <bool F16>
-__device__ __forceinline__ uint32_t pack2(float a, float b)
-{
-    if constexpr (F16) {
-        const __half2 h = __floats2half2_rn(a, b);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    } else {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-}
-
 // floor(log2 r) of a range, kept within what the scaled weights and their sums can take.
 __device__ __forceinline__ float range_exponent(float r)
 {
@@ -131,26 +90,16 @@ __device__ __forceinline__ float range_exponent(float r)
 }
 
 // One request's share of the line of steps.
-struct Request {
-    int32_t q0, n;           // first token, tokens
-    int64_t kv;              // cached tokens
-    int64_t hi;              // keys below this exist
+struct Share : Request {
     int32_t lo_step;         // first step any of its tokens sees
     int32_t steps;           // steps per segment (at least one, so that empty rows are answered)
     int32_t blocks;          // segments per kv head (tokens x query heads fit 31 bits)
 };
 
-__device__ __forceinline__ Request load_request(const KvAttendParams& p, int64_t r, int nc)
+__device__ __forceinline__ Share load_share(const KvAttendParams& p, int64_t r, int nc)
 {
-    Request q;
-    int64_t a = p.q_start[r], b = p.q_start[r + 1];
-    a = a < 0 ? 0 : a > p.tokens ? p.tokens : a;
-    b = b < a ? a : b > p.tokens ? p.tokens : b;
-    q.q0 = (int32_t)a;
-    q.n = (int32_t)(b - a);
-    q.kv = p.kv_len[r] > 0 ? p.kv_len[r] : 0;
-    const int64_t room = p.table_width << p.page_shift;
-    q.hi = q.kv < room ? q.kv : room;
+    Share q;
+    static_cast<Request&>(q) = load_request(p, r);
     const int64_t first = q.kv - q.n;
     int64_t lo = p.window > 0 ? first - p.window + 1 : 0;
     lo = lo < 0 ? 0 : lo;
@@ -158,11 +107,12 @@ __device__ __forceinline__ Request load_request(const KvAttendParams& p, int64_t
     const int64_t st = (q.hi + kStep - 1) / kStep - q.lo_step;
     q.steps = st < 1 ? 1 : (int32_t)st;
     if (st < 1) q.lo_step = 0;               // no key is seen: one step, hidden whole, inside the table
-    q.blocks = (int32_t)(((int64_t)q.n * p.group + nc - 1) / nc);
+    const int64_t rows = (int64_t)q.n * p.group;
+    q.blocks = rows > p.tile_rows ? 0 : (int32_t)((rows + nc - 1) / nc);
     return q;
 }
 
-__device__ __forceinline__ int64_t weight_of(const KvAttendParams& p, const Request& q)
+__device__ __forceinline__ int64_t weight_of(const KvAttendParams& p, const Share& q)
 {
     return (int64_t)q.blocks * p.heads * q.steps;
 }
@@ -241,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
 
     // this CTA's piece [f, f_end) of the line, and the request it starts in
     int64_t total = 0;
-    for (int64_t r = tid; r < p.requests; r += kThreads) total += weight_of(p, load_request(p, r, NC));
+    for (int64_t r = tid; r < p.requests; r += kThreads) total += weight_of(p, load_share(p, r, NC));
     total = warp_sum(total);
     if (lane == 0) scratch[warp] = total;
     __syncthreads();
@@ -257,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
         int64_t before = 0;
         for (int64_t base = 0; base < p.requests; base += kThreads) {
             const int64_t r = base + tid;
-            const int64_t w = r < p.requests ? weight_of(p, load_request(p, r, NC)) : 0;
+            const int64_t w = r < p.requests ? weight_of(p, load_share(p, r, NC)) : 0;
             int64_t incl = w;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -284,16 +234,16 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
         __syncthreads();
     }
     int64_t r = scratch[kWarps], line0 = scratch[kWarps + 1];
-    Request rq = load_request(p, r, NC);
+    Share rq = load_share(p, r, NC);
 
     const uint32_t lane4 = 4u * lane;
-    uint32_t* counters = reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(p.ws) + kWorkspaceBytes);
-    float* parts = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(p.ws) + kWorkspaceBytes + kCounterBytes);
+    uint32_t* counters = p.counters;
+    float* parts = p.parts;
 
     while (f < f_end) {
         while (f >= line0 + weight_of(p, rq)) {      // next request that has queries
             line0 += weight_of(p, rq);
-            rq = load_request(p, ++r, NC);
+            rq = load_share(p, ++r, NC);
         }
         const int64_t seg = (f - line0) / rq.steps;
         const int64_t seg0 = line0 + seg * rq.steps, seg1 = seg0 + rq.steps;
@@ -617,24 +567,17 @@ cudaError_t launch_attend(const KvAttendParams& p, cudaStream_t s)
 }
 
 template <int D, bool F16>
-cudaError_t launch_for(const KvAttendParams& p, int64_t max_q, cudaStream_t s)
+cudaError_t launch_for(const KvAttendParams& p, int64_t max_rows, cudaStream_t s)
 {
-    return max_q * p.group <= 8 ? launch_attend<D, F16, 1>(p, s) : launch_attend<D, F16, 2>(p, s);
+    return max_rows <= 8 ? launch_attend<D, F16, 1>(p, s) : launch_attend<D, F16, 2>(p, s);
 }
 
 }  // namespace
 
-size_t kv_attention_workspace_bytes(int head_dim)
+cudaError_t launch_kv_attend_small(const KvAttendParams& p, int head_dim, bool f16, int64_t max_rows, cudaStream_t s)
 {
-    const int sms = sm_count() > 0 ? sm_count() : 148;
-    const int ctas = sms * kMaxCtasPerSm < kMaxCtas ? sms * kMaxCtasPerSm : kMaxCtas;
-    return kWorkspaceBytes + kCounterBytes + (size_t)2 * ctas * slot_floats(head_dim) * sizeof(float);
-}
-
-cudaError_t launch_kv_attention(const KvAttendParams& p, int head_dim, bool f16, int64_t max_q, cudaStream_t s)
-{
-    if (head_dim == 128) return f16 ? launch_for<128, true>(p, max_q, s) : launch_for<128, false>(p, max_q, s);
-    return f16 ? launch_for<64, true>(p, max_q, s) : launch_for<64, false>(p, max_q, s);
+    if (head_dim == 128) return f16 ? launch_for<128, true>(p, max_rows, s) : launch_for<128, false>(p, max_rows, s);
+    return f16 ? launch_for<64, true>(p, max_rows, s) : launch_for<64, false>(p, max_rows, s);
 }
 
 }  // namespace logq

@@ -63,15 +63,31 @@ struct KvAttendParams {
     float scale_log2;        // scale * log2(e): the softmax runs in base 2
     int32_t pad_;
     int64_t window;          // 0: none
+    int64_t tile_rows;       // requests with more query rows (tokens x group) than this run on the tensor-memory kernel
     uint16_t* out;
     Workspace* ws;
+    uint32_t* counters;      // arrivals at a segment shared by several CTAs, by its first CTA
+    float* parts;            // partial results
     uint16_t k_lvl[16];      // in the cache's type
     uint16_t v_lvl[16];      // in fp16, whatever the cache's type
 };
 
 cudaError_t launch_kv_plan(const KvPlanParams& p, cudaStream_t s);
 cudaError_t launch_kv_append(const KvAppendParams& p, int head_dim, bool f16, cudaStream_t s);
-size_t kv_attention_workspace_bytes(int head_dim);
-cudaError_t launch_kv_attention(const KvAttendParams& p, int head_dim, bool f16, int64_t max_q, cudaStream_t s);
+// Workspace of the attention: record | arrival counters of the small and of the
+// large kernel | partial results of each, two slots per CTA.
+constexpr int kMaxCtasPerSm = 2;             // small kernel
+constexpr int kMaxCols = 16;                 // its query rows per segment, at most
+constexpr int kMaxCtas = 1024;
+constexpr int kTileRows = 256;               // the large kernel's query rows per segment
+constexpr int kTileWarps = 8;                // its warps that hold query rows (32 each) and join parts by themselves
+constexpr size_t kCounterBytes = (size_t)kMaxCtas * (1 + kTileWarps) * sizeof(uint32_t);
+__host__ __device__ constexpr size_t slot_floats(int d) { return (size_t)kMaxCols * (d + 2); }
+__host__ __device__ constexpr size_t tile_slot_floats(int d) { return (size_t)kTileRows * (d + 2); }
+
+// Requests with few query rows: mma.sync, the rows as columns of its tiles.
+cudaError_t launch_kv_attend_small(const KvAttendParams& p, int head_dim, bool f16, int64_t max_rows, cudaStream_t s);
+// Requests with many: tcgen05, 256 rows a segment.
+cudaError_t launch_kv_attend_tiles(const KvAttendParams& p, int head_dim, bool f16, cudaStream_t s);
 
 }  // namespace logq

@@ -1,0 +1,64 @@
+// Device code shared by the two attention kernels of the 4-bit key/value cache.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "kv_cache.h"
+
+namespace logq {
+
+// The softmax runs against a reference value per row, raised when a score
+// exceeds it by 2^kRaise; nothing is subtracted from -inf.
+constexpr float kRefInit = -3.0e38f;
+constexpr float kRaise = 8.0f;
+
+__device__ __forceinline__ float exp2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <bool F16>
+__device__ __forceinline__ float to_float(uint32_t b)
+{
+    if constexpr (F16) return __half2float(__ushort_as_half((unsigned short)b));
+    else return __uint_as_float(b << 16);
+}
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if constexpr (F16) {
+        const __half2 h = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+}
+
+// A request as the attention kernels see it, its lengths made safe to index with.
+struct Request {
+    int32_t q0, n;           // first token, tokens
+    int64_t kv;              // cached tokens
+    int64_t hi;              // keys below this exist
+};
+
+__device__ __forceinline__ Request load_request(const KvAttendParams& p, int64_t r)
+{
+    Request q;
+    int64_t a = p.q_start[r], b = p.q_start[r + 1];
+    a = a < 0 ? 0 : a > p.tokens ? p.tokens : a;
+    b = b < a ? a : b > p.tokens ? p.tokens : b;
+    q.q0 = (int32_t)a;
+    q.n = (int32_t)(b - a);
+    q.kv = p.kv_len[r] > 0 ? p.kv_len[r] : 0;
+    const int64_t room = p.table_width << p.page_shift;
+    q.hi = q.kv < room ? q.kv : room;
+    return q;
+}
+
+}  // namespace logq

@@ -57,6 +57,45 @@ logq_status status_of(cudaError_t e)
     return e == cudaSuccess ? LOGQ_OK : LOGQ_ERR_CUDA;
 }
 
+// Requests with at most this many query rows (tokens x query heads per kv head)
+// run on the small kernel, which re-reads the keys for every 16 of them; the
+// tiles of the large one hold 256.
+constexpr int64_t kTileMinRows = 64;
+
+int sms_or_default() { return sm_count() > 0 ? sm_count() : 148; }
+
+size_t small_parts_offset() { return kWorkspaceBytes + kCounterBytes; }
+
+size_t small_parts_bytes(int head_dim)
+{
+    const int n = sms_or_default() * kMaxCtasPerSm;
+    return (size_t)2 * (n < kMaxCtas ? n : kMaxCtas) * slot_floats(head_dim) * sizeof(float);
+}
+
+size_t tile_parts_bytes(int head_dim)
+{
+    const int n = sms_or_default();
+    return (size_t)2 * (n < kMaxCtas ? n : kMaxCtas) * tile_slot_floats(head_dim) * sizeof(float);
+}
+
+cudaError_t launch_kv_attention(KvAttendParams p, int head_dim, bool f16, int64_t max_q, cudaStream_t s)
+{
+    uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
+    uint32_t* counters = reinterpret_cast<uint32_t*>(ws + kWorkspaceBytes);
+    const bool tiles = max_q > kTileMinRows / p.group;
+    p.tile_rows = tiles ? kTileMinRows : INT64_MAX;
+    if (tiles) {
+        p.counters = counters + kMaxCtas;
+        p.parts = reinterpret_cast<float*>(ws + small_parts_offset() + small_parts_bytes(head_dim));
+        const cudaError_t e = launch_kv_attend_tiles(p, head_dim, f16, s);
+        if (e != cudaSuccess) return e;
+    }
+    p.counters = counters;
+    p.parts = reinterpret_cast<float*>(ws + small_parts_offset());
+    const int64_t max_rows = tiles ? kTileMinRows : max_q * p.group;
+    return launch_kv_attend_small(p, head_dim, f16, max_rows, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -156,7 +195,7 @@ size_t logq_kv_attention_workspace_bytes(int32_t q_heads, int32_t kv_heads, int3
     if (kv_heads < 1 || kv_heads > 1024 || q_heads < kv_heads || q_heads > 65536 || q_heads % kv_heads ||
         !supported_dim(head_dim))
         return 0;
-    return kv_attention_workspace_bytes(head_dim);
+    return small_parts_offset() + small_parts_bytes(head_dim) + tile_parts_bytes(head_dim);
 }
 
 logq_status logq_kv_attention(const logq_kv_cache* cache, const void* q, int64_t q_stride, int32_t q_heads,

@@ -1,0 +1,768 @@
+// Attention over the paged 4-bit key/value cache for requests with many query
+// rows (prompts and their pieces), on the tensor cores.
+//
+// A segment is 256 query rows (tokens x query heads of a group) of one request
+// and kv head, as two tiles of 128 that share every decoded key and value; its
+// keys go by in tiles of 64.  Per key tile and row tile
+//   S = Q K^T          tcgen05.mma M = 128, N = 64,  A = Q from tensor memory
+//   W = 2^(S * scale * range_k + log2 range_v - ref), rounded to fp16
+//   O += W V           tcgen05.mma M = 128, N = D,   A = W from tensor memory
+//   l += W / range_v
+// with K and V decoded to 16-bit levels in shared memory and the ranges kept out
+// of the products, so that only W is rounded.  A row's thread owns the row: the
+// reference is raised (and O rescaled in tensor memory) only when a score
+// exceeds it by 2^8.
+//
+// What bounds it: with A in tensor memory a key tile costs 1024 cycles of MMA at
+// D = 128, and shared memory about as much (operands 512, decoded values written
+// 256, pair-table lookups 256, ranges), so the two row tiles alternate: while one
+// is in its softmax the tensor cores work for the other.  With Q in shared
+// memory its re-reads alone would take 512 cycles a key tile.
+//
+// Tensor memory: S0 S1 (64 columns each; W overwrites the first half of its S)
+// | Q0 Q1 (64 each) | O0 O1 (128 each).
+// Warps: 0-3 and 4-7 softmax of row tile 0 and 1 (a thread per row; they also
+// load Q and write the results), 8-11 decode, 12 issues the MMAs.
+//
+// Split: as in the small kernel the segments' key tiles form one line that the
+// CTAs cut evenly; the last warp to arrive joins the parts of its 32 rows.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "internal.h"
+#include "kv_cache.h"
+#include "kv_device.h"
+#include "ptx.h"
+
+namespace logq {
+namespace {
+
+constexpr int kN = 64;                           // keys per tile
+constexpr int kDecWarp0 = 8, kDecWarps = 4, kMmaWarp = 12;
+constexpr int kThreads = 32 * 16;                // the last three warps only complete the warpgroup
+// Registers per thread: 128 at launch; the softmax warps take what the others give back (2 x 168 + 88 + 88 = 4 x 128).
+constexpr int kRegsSoftmax = 168, kRegsDecode = 88, kRegsMma = 88;
+constexpr int kStages = 8;                       // decoded K / V tiles
+constexpr int kSlots = 4;                        // tiles' ranges
+constexpr int kMinTiles = 4;                     // key tiles per CTA, at least
+constexpr uint32_t kTabBytes = 256 * 256;        // pair tables: keys in the first, values in the second half of a row
+constexpr uint32_t kStageBytes = kN * 256;       // D = 128; D = 64 uses half
+constexpr uint32_t kSlotBytes = 3 * kN * 4;      // range_k * scale, log2 range_v, 1 / range_v
+constexpr uint32_t kStage0 = kTabBytes, kSlot0 = kStage0 + kStages * kStageBytes, kBar0 = kSlot0 + kSlots * kSlotBytes;
+constexpr uint32_t kSmemBytes = kBar0 + 1024;
+constexpr uint32_t kColS = 0, kColQ = 128, kColO = 256, kTmemCols = 512;
+enum : uint32_t { kWaitMma = 0x100, kWaitSoftmax = 0x101, kWaitDecode = 0x102, kWaitDrain = 0x103 };
+
+// A piece of a segment: key tiles [j0, j1) of `tiles`.
+struct Piece {
+    Request rq;
+    int64_t r;
+    int64_t line0;           // the segment's first tile on the line
+    int32_t block, blocks, head;
+    int32_t lo_tile, tiles;
+    int32_t j0, j1;
+};
+
+__device__ __forceinline__ int blocks_of(const KvAttendParams& p, const Request& q)
+{
+    const int64_t rows = (int64_t)q.n * p.group;
+    return rows > p.tile_rows ? (int)((rows + kTileRows - 1) / kTileRows) : 0;
+}
+
+// First key tile and number of key tiles that some row of the block sees (at least one, inside the table).
+__device__ __forceinline__ void block_tiles(const KvAttendParams& p, const Request& q, int block, int* lo_tile, int* tiles)
+{
+    const int row0 = block * kTileRows;
+    int rows = q.n * p.group - row0;
+    rows = rows < kTileRows ? rows : kTileRows;
+    const int64_t first = q.kv - q.n + row0 / p.group, last = q.kv - q.n + (row0 + rows - 1) / p.group;
+    int64_t lo = p.window > 0 ? first - p.window + 1 : 0;
+    lo = lo < 0 ? 0 : lo;
+    const int64_t hi = last + 1 < q.hi ? last + 1 : q.hi;
+    const int64_t t0 = lo / kN, t1 = (hi + kN - 1) / kN;
+    *lo_tile = t1 > t0 ? (int)t0 : 0;
+    *tiles = t1 > t0 ? (int)(t1 - t0) : 1;
+}
+
+// The pieces of this CTA in order.  All roles walk them alike.
+struct Walk {
+    Piece c;
+    int64_t f, f_end;
+
+    __device__ __forceinline__ void set(const KvAttendParams& p)
+    {
+        block_tiles(p, c.rq, c.block, &c.lo_tile, &c.tiles);
+    }
+    __device__ __forceinline__ void clip()
+    {
+        c.j0 = (int)(f - c.line0);
+        c.j1 = f_end - c.line0 < c.tiles ? (int)(f_end - c.line0) : c.tiles;
+    }
+    // The next piece; false at the end of the CTA's share.
+    __device__ __forceinline__ bool next(const KvAttendParams& p)
+    {
+        f = c.line0 + c.j1;
+        if (f >= f_end) return false;
+        c.line0 += c.tiles;
+        if (++c.head == p.heads) {
+            c.head = 0;
+            if (++c.block == c.blocks) {
+                c.block = 0;
+                do {
+                    c.rq = load_request(p, ++c.r);
+                    c.blocks = blocks_of(p, c.rq);
+                } while (c.blocks == 0);
+            }
+            set(p);
+        }
+        clip();
+        return true;
+    }
+};
+
+// 64 consecutive columns of this warp's 32 lanes, complete on return.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&r)[64])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+          "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
+          "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+          "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31]),
+          "=f"(r[32]), "=f"(r[33]), "=f"(r[34]), "=f"(r[35]), "=f"(r[36]), "=f"(r[37]), "=f"(r[38]), "=f"(r[39]),
+          "=f"(r[40]), "=f"(r[41]), "=f"(r[42]), "=f"(r[43]), "=f"(r[44]), "=f"(r[45]), "=f"(r[46]), "=f"(r[47]),
+          "=f"(r[48]), "=f"(r[49]), "=f"(r[50]), "=f"(r[51]), "=f"(r[52]), "=f"(r[53]), "=f"(r[54]), "=f"(r[55]),
+          "=f"(r[56]), "=f"(r[57]), "=f"(r[58]), "=f"(r[59]), "=f"(r[60]), "=f"(r[61]), "=f"(r[62]), "=f"(r[63])
+        : "r"(taddr)
+        : "memory");
+}
+
+__device__ __forceinline__ float4 lds_f4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+
+// Shared-memory descriptor of a [keys][64 dimensions] tile, 128-byte rows, 128-byte
+// swizzle, read with the dimensions along N: 64-dimension groups are `group` bytes
+// apart (leading byte offset), groups of eight keys 1024 (stride byte offset).
+__device__ __forceinline__ uint64_t desc_values(uint32_t addr, uint32_t group)
+{
+    return (smem_desc_sw128(addr) & ~((uint64_t)0x3fff << 16)) | (uint64_t)(group >> 4) << 16;
+}
+
+template <int D, bool F16>
+__global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constant__ KvAttendParams p)
+{
+    constexpr uint32_t kBlockBytes = kN * 128;       // a 64-dimension block of a decoded tile
+    // instruction descriptors: fp32 accumulator, A and B of one type, M = 128
+    constexpr uint32_t kIdescS = (1u << 4) | (F16 ? 0u : (1u << 7 | 1u << 10)) | (uint32_t)(kN >> 3) << 17 | (128u >> 4) << 24;
+    constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | (uint32_t)(D >> 3) << 17 | (128u >> 4) << 24;     // B along N
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t sbase = smem_u32(smem);
+    const uint32_t bar0 = sbase + kBar0;
+    auto full = [&](int s) { return bar0 + 8u * s; };                       // decode -> MMA
+    auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
+    constexpr uint32_t kB1 = 2 * kStages;
+    auto rfull = [&](int s) { return bar0 + 8u * (kB1 + s); };              // decode -> softmax: ranges
+    auto rempty = [&](int s) { return bar0 + 8u * (kB1 + kSlots + s); };
+    constexpr uint32_t kB2 = kB1 + 2 * kSlots;
+    auto sfull = [&](int t) { return bar0 + 8u * (kB2 + t); };              // MMA -> softmax: S
+    auto wfull = [&](int t) { return bar0 + 8u * (kB2 + 2 + t); };          // softmax -> MMA: W
+    auto qfull = [&](int t) { return bar0 + 8u * (kB2 + 4 + t); };          // softmax -> MMA: Q of the next piece
+    auto ofull = [&](int t) { return bar0 + 8u * (kB2 + 6 + t); };          // MMA -> softmax: the piece's O
+    auto oempty = [&](int t) { return bar0 + 8u * (kB2 + 8 + t); };
+    const uint32_t drainb = bar0 + 8u * (kB2 + 10);
+    const uint32_t tmem_slot = bar0 + 8u * (kB2 + 11);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + (tmem_slot + 8 - sbase));
+    int64_t* sched = reinterpret_cast<int64_t*>(smem + (tmem_slot + 16 - sbase));   // [24]
+    static_assert(8 * (kB2 + 12) + 16 + 8 * 24 <= 1024, "barrier block overflows");
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) { mbar_init(full(s), kDecWarps); mbar_init(empty(s), 1); }
+        for (int s = 0; s < kSlots; ++s) { mbar_init(rfull(s), kDecWarps); mbar_init(rempty(s), kTileWarps); }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(sfull(t), 1);
+            mbar_init(wfull(t), 4);
+            mbar_init(qfull(t), 4);
+            mbar_init(ofull(t), 1);
+            mbar_init(oempty(t), 4);
+        }
+        mbar_init(drainb, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    for (int i = tid; i < 256 * 16; i += kThreads) {
+        const int e = i >> 4, part = i & 15;
+        const uint16_t* lv = part < 8 ? p.k_lvl : p.v_lvl;
+        const uint32_t v = (uint32_t)lv[e & 15] | ((uint32_t)lv[e >> 4] << 16);
+        sts128(sbase + e * 256 + part * 16, v, v, v, v);
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---------------- this CTA's piece of the line ----------------
+    // A warp takes 32 requests, then sums each one's blocks with all lanes.
+    auto request_weight = [&](int64_t base) -> int64_t {
+        const int64_t r = base + tid;
+        Request q;
+        q.n = 0;
+        int blocks = 0;
+        if (r < p.requests) {
+            q = load_request(p, r);
+            blocks = blocks_of(p, q);
+        }
+        int64_t weight = 0;
+        for (uint32_t todo = __ballot_sync(0xffffffffu, blocks > 0); todo; todo &= todo - 1) {
+            const int src = __ffs(todo) - 1;
+            Request x;
+            x.q0 = 0;
+            x.n = __shfl_sync(0xffffffffu, q.n, src);
+            x.kv = __shfl_sync(0xffffffffu, q.kv, src);
+            x.hi = __shfl_sync(0xffffffffu, q.hi, src);
+            const int nb = __shfl_sync(0xffffffffu, blocks, src);
+            int64_t sum = 0;
+            for (int b = lane; b < nb; b += 32) {
+                int lo, n;
+                block_tiles(p, x, b, &lo, &n);
+                sum += n;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == src) weight = sum * p.heads;
+        }
+        return weight;
+    };
+    int64_t total = 0;
+    for (int64_t base = 0; base < p.requests; base += kThreads) total += request_weight(base);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (lane == 0) sched[warp] = total;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) total += sched[w];
+    int64_t chunk = (total + gridDim.x - 1) / gridDim.x;
+    chunk = chunk < kMinTiles ? kMinTiles : chunk;
+    Walk walk;
+    walk.f = (int64_t)blockIdx.x * chunk;
+    walk.f_end = walk.f + chunk < total ? walk.f + chunk : total;
+    if (walk.f >= walk.f_end) return;                // the whole CTA
+    int64_t before = 0;
+    for (int64_t base = 0; base < p.requests; base += kThreads) {
+        const int64_t w = request_weight(base);
+        int64_t incl = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += u;
+        }
+        __syncthreads();
+        if (lane == 31) sched[warp] = incl;
+        __syncthreads();
+        int64_t all = 0;
+        for (int x = 0; x < kThreads / 32; ++x) {
+            if (x < warp) incl += sched[x];
+            all += sched[x];
+        }
+        const int64_t from = before + incl - w;
+        if (w > 0 && from <= walk.f && walk.f < from + w) {
+            sched[20] = base + tid;
+            sched[21] = from;
+        }
+        before += all;
+        if (walk.f < before) break;                  // the same for every thread
+    }
+    __syncthreads();
+    walk.c.r = sched[20];
+    walk.c.line0 = sched[21];
+    walk.c.rq = load_request(p, walk.c.r);
+    walk.c.blocks = blocks_of(p, walk.c.rq);
+    {
+        // the block and head that hold f: every warp finds them, 32 blocks at a time
+        int64_t at = walk.c.line0;
+        for (int b0 = 0;; b0 += 32) {
+            int lo, n = 0;
+            if (b0 + lane < walk.c.blocks) block_tiles(p, walk.c.rq, b0 + lane, &lo, &n);
+            int64_t incl = (int64_t)n * p.heads;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += u;
+            }
+            const uint32_t past = __ballot_sync(0xffffffffu, walk.f < at + incl);
+            if (past) {
+                const int src = __ffs(past) - 1;
+                const int64_t line = at + __shfl_sync(0xffffffffu, incl - (int64_t)n * p.heads, src);
+                const int tiles = __shfl_sync(0xffffffffu, n, src);
+                walk.c.block = b0 + src;
+                walk.c.head = (int)((walk.f - line) / tiles);
+                walk.c.line0 = line + (int64_t)walk.c.head * tiles;
+                break;
+            }
+            at += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        walk.set(p);
+        walk.clip();
+    }
+
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + (tmem_slot - sbase));
+
+    if (warp >= kMmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsMma));
+        if (warp == kMmaWarp) {
+        // ---------------- MMA issuer ----------------
+        int stage = 0;
+        uint32_t ph = 0;                             // decoded tiles, in the order K(j), V(j), K(j + 1), ...
+        uint32_t n_piece = 0, n_w = 0;
+        bool ok = true;
+        auto wait_stage = [&]() { ok = ok && warp_wait_inline(full(stage), ph, abort_flag, p.ws, kWaitMma); };
+        auto mma_s = [&](int t, int st) {
+            if (elect_one()) {
+                const uint32_t kb = sbase + kStage0 + st * kStageBytes;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    mma_f16_ta(tmem + kColS + kN * t, tmem + kColQ + 64 * t + 8 * k,
+                               smem_desc_sw128(kb + (k / 4) * kBlockBytes) + 2 * (k % 4), kIdescS, k != 0);
+                mma_commit(sfull(t));
+            }
+            __syncwarp();
+        };
+        auto advance = [&]() { if (++stage == kStages) { stage = 0; ph ^= 1u; } };
+        do {
+            const int n = walk.c.j1 - walk.c.j0;
+            int ks = 0;
+            wait_stage();
+            ks = stage;
+            for (int t = 0; t < 2 && ok; ++t) {
+                ok = warp_wait_inline(qfull(t), n_piece & 1u, abort_flag, p.ws, kWaitMma);
+                if (!ok) break;
+                tc_fence_after();
+                mma_s(t, ks);
+            }
+            if (!ok) break;
+            if (elect_one()) mma_commit(empty(ks));
+            __syncwarp();
+            advance();
+            for (int j = 0; j < n && ok; ++j, ++n_w) {
+                wait_stage();                        // V(j)
+                const int vs = stage;
+                advance();
+                for (int t = 0; t < 2 && ok; ++t) {
+                    ok = ok && warp_wait_inline(wfull(t), n_w & 1u, abort_flag, p.ws, kWaitMma);
+                    if (j == 0) ok = ok && warp_wait_inline(oempty(t), (n_piece & 1u) ^ 1u, abort_flag, p.ws, kWaitMma);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t vb = sbase + kStage0 + vs * kStageBytes;
+#pragma unroll
+                        for (int k = 0; k < kN / 16; ++k)
+                            mma_f16_ta(tmem + kColO + 128 * t, tmem + kColS + kN * t + 8 * k,
+                                       desc_values(vb, kBlockBytes) + 128 * k, kIdescO, j != 0 || k != 0);
+                        if (t == 1) mma_commit(empty(vs));
+                        if (j + 1 == n) mma_commit(ofull(t));
+                    }
+                    __syncwarp();
+                    if (j + 1 < n) {
+                        // the next S of this row tile overwrites W behind the product that reads it
+                        if (t == 0) { wait_stage(); ks = stage; }
+                        if (!ok) break;
+                        tc_fence_after();
+                        mma_s(t, ks);
+                        if (t == 1) {
+                            if (elect_one()) mma_commit(empty(ks));
+                            __syncwarp();
+                            advance();
+                        }
+                    }
+                }
+            }
+            ++n_piece;
+        } while (ok && walk.next(p));
+        }
+    } else if (warp < kTileWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+        // ---------------- softmax, one thread per query row ----------------
+        const int t = warp >> 2;                     // row tile
+        const int row_in = t * 128 + (warp & 3) * 32 + lane;
+        const uint32_t tq = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t ts = tq + kColS + kN * t, to = tq + kColO + 128 * t;
+        int slot = 0;
+        uint32_t rph = 0, n_s = 0, n_piece = 0;
+        bool ok = true;
+        auto load_q = [&]() {
+            const Piece& c = walk.c;
+            const int row = c.block * kTileRows + row_in;
+            const bool live = row < c.rq.n * p.group;
+            const uint16_t* src = p.q + (int64_t)(c.rq.q0 + row / p.group) * p.q_stride +
+                                  (int64_t)(c.head * p.group + row % p.group) * D;
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h) {
+                uint32_t x[32];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (live) v = __ldg(reinterpret_cast<const uint4*>(src + 64 * h) + i);
+                    x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+                }
+                tmem_st_pairs(tq + kColQ + 64 * t + 32 * h, x);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(qfull(t));
+        };
+        load_q();
+        for (;;) {
+            const Piece c = walk.c;
+            const int row = c.block * kTileRows + row_in;
+            const int64_t pos = c.rq.kv - c.rq.n + row / p.group;
+            // keys this row sees: [klo, khi); those that all rows of its tile see need no mask
+            const int64_t khi = pos + 1 < c.rq.hi ? pos + 1 : c.rq.hi;
+            const int64_t klo = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;
+            const int64_t tile_first = c.rq.kv - c.rq.n + (c.block * kTileRows + t * 128) / p.group;
+            const int64_t tile_last = c.rq.kv - c.rq.n + (c.block * kTileRows + t * 128 + 127) / p.group;
+            const int64_t all_hi = tile_first + 1, all_lo = p.window > 0 ? tile_last - p.window + 1 : 0;
+            float ref = kRefInit, sum = 0.0f;
+            for (int j = c.j0; j < c.j1; ++j) {
+                const int64_t kb = (int64_t)(c.lo_tile + j) * kN;
+                if (!warp_wait_inline(rfull(slot), rph, abort_flag, p.ws, kWaitSoftmax) ||
+                    !warp_wait_inline(sfull(t), n_s & 1u, abort_flag, p.ws, kWaitSoftmax)) {
+                    ok = false;
+                    break;
+                }
+                ++n_s;
+                tc_fence_after();
+                const uint32_t rg = sbase + kSlot0 + slot * kSlotBytes;
+                float v[kN];
+                tmem_ld64(ts, v);
+                float top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < kN; i += 4) {
+                    const float4 k4 = lds_f4(rg + 4 * i), l4 = lds_f4(rg + 4 * kN + 4 * i);
+                    v[i] = fmaf(v[i], k4.x, l4.x);
+                    v[i + 1] = fmaf(v[i + 1], k4.y, l4.y);
+                    v[i + 2] = fmaf(v[i + 2], k4.z, l4.z);
+                    v[i + 3] = fmaf(v[i + 3], k4.w, l4.w);
+                }
+                const bool masked = kb + kN > all_hi || kb < all_lo;
+                if (masked) {
+                    const int a = klo > kb ? (int)(klo - kb < kN ? klo - kb : kN) : 0;
+                    const int b = khi > kb ? (int)(khi - kb < kN ? khi - kb : kN) : 0;
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) v[i] = i >= a && i < b ? v[i] : -INFINITY;
+                }
+#pragma unroll
+                for (int i = 0; i < kN; ++i) top = fmaxf(top, v[i]);
+                if (__any_sync(0xffffffffu, top > ref + kRaise)) {
+                    const float to_ref = fmaxf(ref, top);
+                    const float f = exp2_approx(ref - to_ref);
+                    ref = to_ref;
+                    sum *= f;
+                    if (j != c.j0) {                 // O holds the products of all earlier key tiles
+#pragma unroll 1
+                        for (int h = 0; h < D / 32; ++h) {
+                            uint32_t o[32];
+                            tmem_ld32(to + 32 * h, o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st_pairs(to + 32 * h, o);
+                        }
+                    }
+                }
+                uint32_t w[kN / 2];
+                float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kN; i += 4) {
+                    const float4 i4 = lds_f4(rg + 8 * kN + 4 * i);
+                    const float a = exp2_approx(v[i] - ref), b = exp2_approx(v[i + 1] - ref);
+                    const float c2 = exp2_approx(v[i + 2] - ref), d = exp2_approx(v[i + 3] - ref);
+                    if (!masked) {
+                        s0 = fmaf(a, i4.x, s0);
+                        s1 = fmaf(b, i4.y, s1);
+                        s0 = fmaf(c2, i4.z, s0);
+                        s1 = fmaf(d, i4.w, s1);
+                    } else {                         // a hidden key's range may be anything
+                        s0 = v[i] == -INFINITY ? s0 : fmaf(a, i4.x, s0);
+                        s1 = v[i + 1] == -INFINITY ? s1 : fmaf(b, i4.y, s1);
+                        s0 = v[i + 2] == -INFINITY ? s0 : fmaf(c2, i4.z, s0);
+                        s1 = v[i + 3] == -INFINITY ? s1 : fmaf(d, i4.w, s1);
+                    }
+                    w[i / 2] = pack2<true>(a, b);
+                    w[i / 2 + 1] = pack2<true>(c2, d);
+                }
+                sum += s0 + s1;
+                tmem_st_pairs(ts, w);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(wfull(t));
+                    mbar_arrive(rempty(slot));
+                }
+                if (++slot == kSlots) { slot = 0; rph ^= 1u; }
+            }
+            if (!ok) break;
+            // the piece's last S is read, so Q may be replaced and the next piece begin
+            const bool more = walk.next(p);
+            if (more) load_q();
+            if (!warp_wait_inline(ofull(t), n_piece & 1u, abort_flag, p.ws, kWaitSoftmax)) break;
+            ++n_piece;
+            tc_fence_after();
+            const bool whole = c.j0 == 0 && c.j1 == c.tiles;
+            const bool live = row < c.rq.n * p.group;
+            float* part = p.parts + (size_t)(2 * blockIdx.x + (c.j0 == 0 ? 1 : 0)) * tile_slot_floats(D);
+            uint16_t* dst = p.out + ((int64_t)(c.rq.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group +
+                                     row % p.group) * D;
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll 1
+            for (int h = 0; h < D / 32; ++h) {
+                uint32_t o[32];
+                tmem_ld32(to + 32 * h, o);
+                if (whole) {
+                    if (live) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                y[k] = pack2<F16>(__uint_as_float(o[8 * i + 2 * k]) * inv, __uint_as_float(o[8 * i + 2 * k + 1]) * inv);
+                            *(reinterpret_cast<uint4*>(dst + 32 * h) + i) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        __stcg(reinterpret_cast<uint4*>(part + (size_t)row_in * D + 32 * h) + i,
+                               make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(oempty(t));
+            if (!whole) {
+                __stcg(reinterpret_cast<float2*>(part + (size_t)kTileRows * D) + row_in, make_float2(ref, sum));
+                const int64_t seg1 = c.line0 + c.tiles;
+                const int c0 = (int)(c.line0 / chunk), c1 = (int)((seg1 - 1) / chunk);
+                __threadfence();
+                __syncwarp();
+                uint32_t last = 0;
+                if (lane == 0) last = atomicInc(&p.counters[c0 * kTileWarps + warp], (uint32_t)(c1 - c0)) == (uint32_t)(c1 - c0);
+                if (__shfl_sync(0xffffffffu, last, 0)) {
+                    __threadfence();
+                    auto part_of = [&](int x) { return p.parts + (size_t)(2 * x + (x == c0 ? 1 : 0)) * tile_slot_floats(D); };
+                    float m = kRefInit;
+                    for (int x = c0; x <= c1; ++x)
+                        m = fmaxf(m, __ldcg(reinterpret_cast<const float2*>(part_of(x) + (size_t)kTileRows * D) + row_in).x);
+                    float l = 0.0f;
+                    for (int x = c0; x <= c1; ++x) {
+                        const float2 st = __ldcg(reinterpret_cast<const float2*>(part_of(x) + (size_t)kTileRows * D) + row_in);
+                        l += st.y * exp2_approx(st.x - m);
+                    }
+                    const float li = l == 0.0f ? 0.0f : 1.0f / l;
+                    for (int d = 0; d < D && live; d += 8) {
+                        float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                        for (int x = c0; x <= c1; ++x) {
+                            const float* src = part_of(x);
+                            const float k = exp2_approx(__ldcg(reinterpret_cast<const float2*>(src + (size_t)kTileRows * D) + row_in).x - m) * li;
+                            const float4 a = __ldcg(reinterpret_cast<const float4*>(src + (size_t)row_in * D + d));
+                            const float4 b = __ldcg(reinterpret_cast<const float4*>(src + (size_t)row_in * D + d) + 1);
+                            y[0] += a.x * k; y[1] += a.y * k; y[2] += a.z * k; y[3] += a.w * k;
+                            y[4] += b.x * k; y[5] += b.y * k; y[6] += b.z * k; y[7] += b.w * k;
+                        }
+                        *reinterpret_cast<uint4*>(dst + d) = make_uint4(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]),
+                                                                       pack2<F16>(y[4], y[5]), pack2<F16>(y[6], y[7]));
+                    }
+                }
+            }
+            if (!more) break;
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsDecode));
+        // ---------------- decode ----------------
+        // A thread's task: a 16-byte chunk (32 codes) of a key row.  Eight neighbouring
+        // lanes take eight rows of one chunk, so that their swizzled stores fill all banks.
+        constexpr int kChunks = D / 32;              // chunks per row: 4 or 2
+        constexpr int kTasks = kN * kChunks / (32 * kDecWarps);
+        constexpr int kRowsPerWarp = 32 / kChunks;
+        const int dw = warp - kDecWarp0, dt = dw * 32 + lane;
+        const int chunk_i = (lane >> 3) % kChunks;
+        const int row_l = (lane & 7) + 8 * ((lane >> 3) / kChunks);
+        const uint32_t lane4 = 4u * lane;
+        auto task_row = [&](int i) { return (i * kDecWarps + dw) * kRowsPerWarp + row_l; };
+        // A tile whose loads are in flight.
+        struct Tile {
+            int64_t kb, hi;
+            int head;
+            bool any;
+            int32_t page[kTasks], page_r;
+        };
+        Walk ahead = walk;                           // two tiles ahead of the decoding
+        int aj = ahead.c.j0;
+        bool alive = true;
+        const int shift = p.page_shift;
+        auto fetch_pages = [&](Tile& x) {
+            x.any = alive;
+            if (!alive) return;
+            x.kb = (int64_t)(ahead.c.lo_tile + aj) * kN;
+            x.hi = ahead.c.rq.hi;
+            x.head = ahead.c.head;
+            const int32_t* table = p.block_table + ahead.c.r * p.table_width;
+#pragma unroll
+            for (int i = 0; i < kTasks; ++i) {
+                const int64_t key = x.kb + task_row(i);
+                x.page[i] = key < x.hi ? __ldg(table + (key >> shift)) : -1;
+            }
+            const int64_t key = x.kb + dt;
+            x.page_r = dt < kN && key < x.hi ? __ldg(table + (key >> shift)) : -1;
+            if (++aj == ahead.c.j1) {
+                alive = ahead.next(p);
+                aj = ahead.c.j0;
+            }
+        };
+        struct Codes {
+            uint4 k[kTasks], v[kTasks];
+            uint16_t kr, vr;
+            bool real;                               // this thread's key exists
+        };
+        auto fetch_codes = [&](const Tile& x, Codes& c) {
+            if (!x.any) return;
+#pragma unroll
+            for (int i = 0; i < kTasks; ++i) {
+                c.k[i] = c.v[i] = make_uint4(0, 0, 0, 0);
+                if (x.page[i] >= 0 && x.page[i] < p.pages) {
+                    const int64_t key = x.kb + task_row(i);
+                    const int64_t at = (((int64_t)x.page[i] * p.heads + x.head) * p.page_size + (key & (p.page_size - 1))) * (D / 2) + chunk_i * 16;
+                    c.k[i] = __ldg(reinterpret_cast<const uint4*>(p.k_codes + at));
+                    c.v[i] = __ldg(reinterpret_cast<const uint4*>(p.v_codes + at));
+                }
+            }
+            c.real = x.page_r >= 0 && x.page_r < p.pages;
+            c.kr = c.vr = 0;
+            if (c.real) {
+                const int64_t key = x.kb + dt;
+                const int64_t at = ((int64_t)x.page_r * p.heads + x.head) * p.page_size + (key & (p.page_size - 1));
+                c.kr = __ldg(p.k_range + at);
+                c.vr = __ldg(p.v_range + at);
+            }
+        };
+        int stage = 0, slot = 0;
+        uint32_t ph = 0, rph = 0;
+        bool ok = true;
+        // which: this lane's copy of the keys' or of the values' entry, within a table row
+        auto store = [&](uint32_t which, const uint4 (&codes)[kTasks]) {
+            if (!warp_wait_inline(empty(stage), ph ^ 1u, abort_flag, p.ws, kWaitDecode)) {
+                ok = false;
+                return;
+            }
+            const uint32_t base = sbase + kStage0 + stage * kStageBytes;
+#pragma unroll
+            for (int i = 0; i < kTasks; ++i) {
+                const int row = task_row(i);
+                const uint32_t rb = base + (uint32_t)(chunk_i >> 1) * kBlockBytes + (uint32_t)row * 128;
+                const uint32_t x[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t c16 = (uint32_t)((chunk_i & 1) * 4 + q) ^ (uint32_t)(row & 7);
+                    sts128(rb + c16 * 16, lds_tab(prmt(x[q], which, 0x7604u)), lds_tab(prmt(x[q], which, 0x7614u)),
+                           lds_tab(prmt(x[q], which, 0x7624u)), lds_tab(prmt(x[q], which, 0x7634u)));
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // visible to the MMA's reads
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full(stage));
+            if (++stage == kStages) { stage = 0; ph ^= 1u; }
+        };
+        Tile pages;
+        Codes cur, nxt;
+        fetch_pages(pages);
+        fetch_codes(pages, nxt);
+        fetch_pages(pages);
+        int64_t left = walk.f_end - walk.f;
+        for (; left > 0 && ok; --left) {
+            cur = nxt;
+            fetch_codes(pages, nxt);
+            fetch_pages(pages);
+            if (!warp_wait_inline(rempty(slot), rph ^ 1u, abort_flag, p.ws, kWaitDecode)) break;
+            if (dt < kN) {
+                // a range of zero stands for zeros: any small one gives the same products
+                const float vr = to_float<F16>(cur.vr);
+                const uint32_t at = kSlot0 + slot * kSlotBytes + 4 * dt;
+                *reinterpret_cast<float*>(smem + at) = cur.real ? to_float<F16>(cur.kr) * p.scale_log2 : 0.0f;
+                *reinterpret_cast<float*>(smem + at + 4 * kN) = !cur.real ? -INFINITY : vr == 0.0f ? -60.0f : log2f(vr);
+                *reinterpret_cast<float*>(smem + at + 8 * kN) = !cur.real ? 0.0f : vr == 0.0f ? 0x1p60f : 1.0f / vr;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(rfull(slot));
+            if (++slot == kSlots) { slot = 0; rph ^= 1u; }
+            store(lane4, cur.k);
+            if (ok) store(lane4 + 128u, cur.v);
+        }
+    }
+
+    // teardown: every MMA this CTA issued has completed before tensor memory is freed
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        if (elect_one()) mma_commit(drainb);
+        __syncwarp();
+        warp_wait_inline(drainb, 0, abort_flag, p.ws, kWaitDrain, true);
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+template <int D, bool F16>
+cudaError_t launch_tiles(const KvAttendParams& p, cudaStream_t s)
+{
+    static bool configured[64] = {false};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!configured[dev]) {
+        int reserved = 0, optin = 0;
+        if ((e = cudaDeviceGetAttribute(&reserved, cudaDevAttrReservedSharedMemoryPerBlock, dev)) != cudaSuccess) return e;
+        if ((e = cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev)) != cudaSuccess) return e;
+        if (reserved != (int)kTabOff || (int)kSmemBytes > optin) return cudaErrorNotSupported;
+        if ((e = cudaFuncSetAttribute(tiles_kernel<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes)) != cudaSuccess)
+            return e;
+        configured[dev] = true;
+    }
+    const int sms = sm_count() > 0 ? sm_count() : 148;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(sms < kMaxCtas ? sms : kMaxCtas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, tiles_kernel<D, F16>, p);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_attend_tiles(const KvAttendParams& p, int head_dim, bool f16, cudaStream_t s)
+{
+    if (head_dim == 128) return f16 ? launch_tiles<128, true>(p, s) : launch_tiles<128, false>(p, s);
+    return f16 ? launch_tiles<64, true>(p, s) : launch_tiles<64, false>(p, s);
+}
+
+}  // namespace logq
