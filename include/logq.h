@@ -464,6 +464,7 @@ size_t logq_kv_attention_workspace_bytes(int32_t q_heads, int32_t kv_heads, int3
  *   page_size and in pages the cache has:
  *   out = sum_j softmax_j(scale * q . k_j) v_j.  A token that sees no key
  *   (p < 0, kv_len 0) gives zeros.  Tokens outside every request are not written.
+ *   table_width * page_size is at most 2^30.
  *   max_q: an upper bound of a request's tokens in this call; it only chooses
  *   kernels (any value gives the same results up to rounding).
  * Scores, softmax and sums are fp32; the weights that multiply the values are

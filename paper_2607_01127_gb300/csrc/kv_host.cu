@@ -209,7 +209,7 @@ logq_status logq_kv_attention(const logq_kv_cache* cache, const void* q, int64_t
     if (tokens < 0 || tokens > 0x7fffffffll / q_heads || requests < 0 || requests > 0x7ffffffell || max_q < 0 ||
         window < 0 || !isfinite(scale))
         return LOGQ_ERR_INVALID_ARG;
-    if (table_width < 1 || table_width > 0x7fffffffll / cache->page_size) return LOGQ_ERR_INVALID_ARG;
+    if (table_width < 1 || table_width > (int64_t(1) << 30) / cache->page_size) return LOGQ_ERR_INVALID_ARG;
     if (q_stride < (int64_t)q_heads * cache->head_dim || (q_stride & 7) || q_stride > (int64_t(1) << 31))
         return LOGQ_ERR_INVALID_ARG;
     if (!aligned(workspace, 256) ||
@@ -240,7 +240,7 @@ logq_status logq_kv_attention(const logq_kv_cache* cache, const void* q, int64_t
     p.block_table = block_table;
     p.table_width = table_width;
     p.scale_log2 = (float)(scale * 1.4426950408889634);
-    p.window = window;
+    p.window = window <= 0x7fffffffll ? window : 0;      // beyond every position: no limit
     p.out = static_cast<uint16_t*>(out);
     p.ws = static_cast<Workspace*>(workspace);
     for (int c = 0; c < 16; ++c) {

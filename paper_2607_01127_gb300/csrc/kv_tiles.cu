@@ -22,7 +22,8 @@
 // Tensor memory: S0 S1 (64 columns each; W overwrites the first half of its S)
 // | Q0 Q1 (64 each) | O0 O1 (128 each).
 // Warps: 0-3 and 4-7 softmax of row tile 0 and 1 (a thread per row; they also
-// load Q and write the results), 8-11 decode, 12 issues the MMAs.
+// load Q and write the results), 8-11 decode, 12 and 13 issue the MMAs of a row tile
+// each (one warp for both took longer to issue than the tensor cores to run).
 //
 // Split: as in the small kernel the segments' key tiles form one line that the
 // CTAs cut evenly; the last warp to arrive joins the parts of its 32 rows.
@@ -39,31 +40,37 @@
 namespace logq {
 namespace {
 
+// A piece of a segment: key tiles [j0, j1) of it, for all roles to read from shared memory.
+struct Piece {
+    int32_t r, q0, n, kv, hi;        // request: row of the block table, first token, tokens, cached tokens, keys that exist
+    int32_t row0, head;              // first query row, kv head
+    int32_t lo_tile, j0, j1;         // key tiles lo_tile + j; j0 == j1 ends the sequence
+    int32_t whole;                   // the segment is this CTA's alone
+    int32_t cta0, cta1;              // else the CTAs that share it
+    int32_t starts;                  // it begins here (the second of the CTA's two partial slots)
+    int32_t pad_[2];
+};
+static_assert(sizeof(Piece) == 64, "moved as four 16-byte words");
+
 constexpr int kN = 64;                           // keys per tile
-constexpr int kDecWarp0 = 8, kDecWarps = 4, kMmaWarp = 12;
-constexpr int kThreads = 32 * 16;                // the last three warps only complete the warpgroup
-// Registers per thread: 128 at launch; the softmax warps take what the others give back (2 x 168 + 88 + 88 = 4 x 128).
-constexpr int kRegsSoftmax = 168, kRegsDecode = 88, kRegsMma = 88;
+constexpr int kDecWarp0 = 8, kDecWarps = 4, kMmaWarp = 12;     // and 13
+constexpr int kPlanWarp = 14;
+constexpr int kThreads = 32 * 16;                // the last warp only completes the warpgroup
+// Registers per thread: 128 at launch; the softmax warps take what the others give back (2 x 160 + 96 + 96 = 4 x 128).
+constexpr int kRegsSoftmax = 160, kRegsDecode = 96, kRegsMma = 96;
 constexpr int kStages = 8;                       // decoded K / V tiles
 constexpr int kSlots = 4;                        // tiles' ranges
 constexpr int kMinTiles = 4;                     // key tiles per CTA, at least
 constexpr uint32_t kTabBytes = 256 * 256;        // pair tables: keys in the first, values in the second half of a row
 constexpr uint32_t kStageBytes = kN * 256;       // D = 128; D = 64 uses half
 constexpr uint32_t kSlotBytes = 3 * kN * 4;      // range_k * scale, log2 range_v, 1 / range_v
-constexpr uint32_t kStage0 = kTabBytes, kSlot0 = kStage0 + kStages * kStageBytes, kBar0 = kSlot0 + kSlots * kSlotBytes;
+constexpr int kPieces = 4;                       // pieces announced ahead
+constexpr uint32_t kStage0 = kTabBytes, kSlot0 = kStage0 + kStages * kStageBytes, kPiece0 = kSlot0 + kSlots * kSlotBytes;
+constexpr uint32_t kBar0 = kPiece0 + kPieces * sizeof(Piece);
 constexpr uint32_t kSmemBytes = kBar0 + 1024;
 constexpr uint32_t kColS = 0, kColQ = 128, kColO = 256, kTmemCols = 512;
-enum : uint32_t { kWaitMma = 0x100, kWaitSoftmax = 0x101, kWaitDecode = 0x102, kWaitDrain = 0x103 };
-
-// A piece of a segment: key tiles [j0, j1) of `tiles`.
-struct Piece {
-    Request rq;
-    int64_t r;
-    int64_t line0;           // the segment's first tile on the line
-    int32_t block, blocks, head;
-    int32_t lo_tile, tiles;
-    int32_t j0, j1;
-};
+enum : uint32_t { kWaitMma = 0x100, kWaitSoftmax = 0x101, kWaitDecode = 0x102, kWaitDrain = 0x103,
+                  kWaitPlan = 0x104 };
 
 __device__ __forceinline__ int blocks_of(const KvAttendParams& p, const Request& q)
 {
@@ -77,50 +84,13 @@ __device__ __forceinline__ void block_tiles(const KvAttendParams& p, const Reque
     const int row0 = block * kTileRows;
     int rows = q.n * p.group - row0;
     rows = rows < kTileRows ? rows : kTileRows;
-    const int64_t first = q.kv - q.n + row0 / p.group, last = q.kv - q.n + (row0 + rows - 1) / p.group;
-    int64_t lo = p.window > 0 ? first - p.window + 1 : 0;
-    lo = lo < 0 ? 0 : lo;
-    const int64_t hi = last + 1 < q.hi ? last + 1 : q.hi;
-    const int64_t t0 = lo / kN, t1 = (hi + kN - 1) / kN;
-    *lo_tile = t1 > t0 ? (int)t0 : 0;
-    *tiles = t1 > t0 ? (int)(t1 - t0) : 1;
+    const int first = (int)q.kv - q.n + row0 / p.group, last = (int)q.kv - q.n + (row0 + rows - 1) / p.group;
+    const int lo = p.window > 0 && first >= p.window ? first - (int)p.window + 1 : 0;
+    const int hi = last + 1 < (int)q.hi ? last + 1 : (int)q.hi;
+    const int t0 = lo / kN, t1 = hi > 0 ? (hi + kN - 1) / kN : 0;
+    *lo_tile = t1 > t0 ? t0 : 0;
+    *tiles = t1 > t0 ? t1 - t0 : 1;
 }
-
-// The pieces of this CTA in order.  All roles walk them alike.
-struct Walk {
-    Piece c;
-    int64_t f, f_end;
-
-    __device__ __forceinline__ void set(const KvAttendParams& p)
-    {
-        block_tiles(p, c.rq, c.block, &c.lo_tile, &c.tiles);
-    }
-    __device__ __forceinline__ void clip()
-    {
-        c.j0 = (int)(f - c.line0);
-        c.j1 = f_end - c.line0 < c.tiles ? (int)(f_end - c.line0) : c.tiles;
-    }
-    // The next piece; false at the end of the CTA's share.
-    __device__ __forceinline__ bool next(const KvAttendParams& p)
-    {
-        f = c.line0 + c.j1;
-        if (f >= f_end) return false;
-        c.line0 += c.tiles;
-        if (++c.head == p.heads) {
-            c.head = 0;
-            if (++c.block == c.blocks) {
-                c.block = 0;
-                do {
-                    c.rq = load_request(p, ++c.r);
-                    c.blocks = blocks_of(p, c.rq);
-                } while (c.blocks == 0);
-            }
-            set(p);
-        }
-        clip();
-        return true;
-    }
-};
 
 // 64 consecutive columns of this warp's 32 lanes, complete on return.
 __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&r)[64])
@@ -149,13 +119,18 @@ __device__ __forceinline__ float4 lds_f4(uint32_t addr)
     return v;
 }
 
-// Shared-memory descriptor of a [keys][64 dimensions] tile, 128-byte rows, 128-byte
-// swizzle, read with the dimensions along N: 64-dimension groups are `group` bytes
-// apart (leading byte offset), groups of eight keys 1024 (stride byte offset).
-__device__ __forceinline__ uint64_t desc_values(uint32_t addr, uint32_t group)
+// Shared-memory descriptors of a [keys][64 dimensions] tile, 128-byte rows, 128-byte
+// swizzle (ptx.h gives the fields).  Keys are read along K-major rows; for the
+// values the dimensions run along N, 64-dimension groups `group` bytes apart
+// (leading byte offset) and groups of eight keys 1024 (stride byte offset).  The
+// upper words are constants, the lower ones an address and an offset.
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo)
 {
-    return (smem_desc_sw128(addr) & ~((uint64_t)0x3fff << 16)) | (uint64_t)(group >> 4) << 16;
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "n"((1024 >> 4) | 1u << 14 | 2u << 29));
+    return d;
 }
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t group) { return (addr >> 4) | (group >> 4) << 16; }
 
 template <int D, bool F16>
 __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constant__ KvAttendParams p)
@@ -178,15 +153,18 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     auto qfull = [&](int t) { return bar0 + 8u * (kB2 + 4 + t); };          // softmax -> MMA: Q of the next piece
     auto ofull = [&](int t) { return bar0 + 8u * (kB2 + 6 + t); };          // MMA -> softmax: the piece's O
     auto oempty = [&](int t) { return bar0 + 8u * (kB2 + 8 + t); };
-    const uint32_t drainb = bar0 + 8u * (kB2 + 10);
-    const uint32_t tmem_slot = bar0 + 8u * (kB2 + 11);
+    auto pfull = [&](int s) { return bar0 + 8u * (kB2 + 10 + s); };         // planner -> all roles: a piece
+    auto pempty = [&](int s) { return bar0 + 8u * (kB2 + 10 + kPieces + s); };
+    constexpr uint32_t kB3 = kB2 + 10 + 2 * kPieces;
+    const uint32_t drainb = bar0 + 8u * kB3;
+    const uint32_t tmem_slot = bar0 + 8u * (kB3 + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + (tmem_slot + 8 - sbase));
     int64_t* sched = reinterpret_cast<int64_t*>(smem + (tmem_slot + 16 - sbase));   // [24]
-    static_assert(8 * (kB2 + 12) + 16 + 8 * 24 <= 1024, "barrier block overflows");
+    static_assert(8 * (kB3 + 2) + 16 + 8 * 24 <= 1024, "barrier block overflows");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(full(s), kDecWarps); mbar_init(empty(s), 1); }
+        for (int s = 0; s < kStages; ++s) { mbar_init(full(s), kDecWarps); mbar_init(empty(s), 2); }
         for (int s = 0; s < kSlots; ++s) { mbar_init(rfull(s), kDecWarps); mbar_init(rempty(s), kTileWarps); }
         for (int t = 0; t < 2; ++t) {
             mbar_init(sfull(t), 1);
@@ -195,7 +173,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             mbar_init(ofull(t), 1);
             mbar_init(oempty(t), 4);
         }
-        mbar_init(drainb, 1);
+        for (int s = 0; s < kPieces; ++s) { mbar_init(pfull(s), 1); mbar_init(pempty(s), 2 + kTileWarps + kDecWarps); }
+        mbar_init(drainb, 2);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -250,10 +229,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     for (int w = 0; w < kThreads / 32; ++w) total += sched[w];
     int64_t chunk = (total + gridDim.x - 1) / gridDim.x;
     chunk = chunk < kMinTiles ? kMinTiles : chunk;
-    Walk walk;
-    walk.f = (int64_t)blockIdx.x * chunk;
-    walk.f_end = walk.f + chunk < total ? walk.f + chunk : total;
-    if (walk.f >= walk.f_end) return;                // the whole CTA
+    const int64_t f0 = (int64_t)blockIdx.x * chunk, f_end = f0 + chunk < total ? f0 + chunk : total;
+    if (f0 >= f_end) return;                         // the whole CTA
     int64_t before = 0;
     for (int64_t base = 0; base < p.requests; base += kThreads) {
         const int64_t w = request_weight(base);
@@ -272,46 +249,14 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             all += sched[x];
         }
         const int64_t from = before + incl - w;
-        if (w > 0 && from <= walk.f && walk.f < from + w) {
+        if (w > 0 && from <= f0 && f0 < from + w) {
             sched[20] = base + tid;
             sched[21] = from;
         }
         before += all;
-        if (walk.f < before) break;                  // the same for every thread
+        if (f0 < before) break;                      // the same for every thread
     }
     __syncthreads();
-    walk.c.r = sched[20];
-    walk.c.line0 = sched[21];
-    walk.c.rq = load_request(p, walk.c.r);
-    walk.c.blocks = blocks_of(p, walk.c.rq);
-    {
-        // the block and head that hold f: every warp finds them, 32 blocks at a time
-        int64_t at = walk.c.line0;
-        for (int b0 = 0;; b0 += 32) {
-            int lo, n = 0;
-            if (b0 + lane < walk.c.blocks) block_tiles(p, walk.c.rq, b0 + lane, &lo, &n);
-            int64_t incl = (int64_t)n * p.heads;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += u;
-            }
-            const uint32_t past = __ballot_sync(0xffffffffu, walk.f < at + incl);
-            if (past) {
-                const int src = __ffs(past) - 1;
-                const int64_t line = at + __shfl_sync(0xffffffffu, incl - (int64_t)n * p.heads, src);
-                const int tiles = __shfl_sync(0xffffffffu, n, src);
-                walk.c.block = b0 + src;
-                walk.c.head = (int)((walk.f - line) / tiles);
-                walk.c.line0 = line + (int64_t)walk.c.head * tiles;
-                break;
-            }
-            at += __shfl_sync(0xffffffffu, incl, 31);
-        }
-        walk.set(p);
-        walk.clip();
-    }
-
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(kTmemCols)
                      : "memory");
@@ -322,77 +267,154 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + (tmem_slot - sbase));
 
+    // A role's place in the sequence of pieces.
+    struct Reader {
+        int slot;
+        uint32_t ph;
+    };
+    auto read_piece = [&](Reader& q, Piece& c) {
+        const bool ok = warp_wait_inline(pfull(q.slot), q.ph, abort_flag, p.ws, kWaitPlan);
+        const uint32_t src = sbase + kPiece0 + q.slot * (uint32_t)sizeof(Piece);
+        const uint4 a = lds128(src), b = lds128(src + 16), d = lds128(src + 32), e = lds128(src + 48);
+        c.r = (int)a.x; c.q0 = (int)a.y; c.n = (int)a.z; c.kv = (int)a.w;
+        c.hi = (int)b.x; c.row0 = (int)b.y; c.head = (int)b.z; c.lo_tile = (int)b.w;
+        c.j0 = (int)d.x; c.j1 = (int)d.y; c.whole = (int)d.z; c.cta0 = (int)d.w;
+        c.cta1 = (int)e.x; c.starts = (int)e.y;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(pempty(q.slot));
+        if (++q.slot == kPieces) { q.slot = 0; q.ph ^= 1u; }
+        return ok && c.j0 < c.j1;
+    };
+
     if (warp >= kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsMma));
-        if (warp == kMmaWarp) {
-        // ---------------- MMA issuer ----------------
-        int stage = 0;
-        uint32_t ph = 0;                             // decoded tiles, in the order K(j), V(j), K(j + 1), ...
-        uint32_t n_piece = 0, n_w = 0;
-        bool ok = true;
-        auto wait_stage = [&]() { ok = ok && warp_wait_inline(full(stage), ph, abort_flag, p.ws, kWaitMma); };
-        auto mma_s = [&](int t, int st) {
-            if (elect_one()) {
-                const uint32_t kb = sbase + kStage0 + st * kStageBytes;
+        if (warp == kPlanWarp) {
+            // ---------------- planner: the pieces of [f0, f_end) in order ----------------
+            int64_t r = sched[20], line = sched[21];
+            Request rq = load_request(p, r);
+            int blocks = blocks_of(p, rq), block = 0, head = 0, lo_tile = 0, tiles = 0;
+            // the block and head that hold f0, 32 blocks at a time
+            for (int b0 = 0; b0 < blocks; b0 += 32) {
+                int lo, n = 0;
+                if (b0 + lane < blocks) block_tiles(p, rq, b0 + lane, &lo, &n);
+                const int64_t w = (int64_t)n * p.heads;
+                int64_t incl = w;
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    mma_f16_ta(tmem + kColS + kN * t, tmem + kColQ + 64 * t + 8 * k,
-                               smem_desc_sw128(kb + (k / 4) * kBlockBytes) + 2 * (k % 4), kIdescS, k != 0);
-                mma_commit(sfull(t));
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
+                    if (lane >= o) incl += u;
+                }
+                const uint32_t past = __ballot_sync(0xffffffffu, f0 < line + incl);
+                if (past) {
+                    const int src = __ffs(past) - 1;
+                    line += __shfl_sync(0xffffffffu, incl - w, src);
+                    block = b0 + src;
+                    block_tiles(p, rq, block, &lo_tile, &tiles);
+                    head = (int)((f0 - line) / tiles);
+                    line += (int64_t)head * tiles;
+                    break;
+                }
+                line += __shfl_sync(0xffffffffu, incl, 31);
             }
-            __syncwarp();
-        };
-        auto advance = [&]() { if (++stage == kStages) { stage = 0; ph ^= 1u; } };
-        do {
-            const int n = walk.c.j1 - walk.c.j0;
-            int ks = 0;
-            wait_stage();
-            ks = stage;
-            for (int t = 0; t < 2 && ok; ++t) {
-                ok = warp_wait_inline(qfull(t), n_piece & 1u, abort_flag, p.ws, kWaitMma);
-                if (!ok) break;
+            int slot = 0;
+            uint32_t ph = 0;
+            for (int64_t f = f0;;) {
+                if (!warp_wait_inline(pempty(slot), ph ^ 1u, abort_flag, p.ws, kWaitPlan)) break;
+                Piece c{};
+                if (f < f_end) {
+                    const int64_t seg1 = line + tiles;
+                    c.r = (int)r;
+                    c.q0 = rq.q0;
+                    c.n = rq.n;
+                    c.kv = (int)rq.kv;
+                    c.hi = (int)rq.hi;
+                    c.row0 = block * kTileRows;
+                    c.head = head;
+                    c.lo_tile = lo_tile;
+                    c.j0 = (int)(f - line);
+                    c.j1 = (int)((f_end < seg1 ? f_end : seg1) - line);
+                    c.whole = c.j0 == 0 && c.j1 == tiles;
+                    c.cta0 = (int)(line / chunk);
+                    c.cta1 = (int)((seg1 - 1) / chunk);
+                    c.starts = c.j0 == 0;
+                }
+                if (lane == 0) {
+                    const uint32_t dst = sbase + kPiece0 + slot * (uint32_t)sizeof(Piece);
+                    sts128(dst, c.r, c.q0, c.n, c.kv);
+                    sts128(dst + 16, c.hi, c.row0, c.head, c.lo_tile);
+                    sts128(dst + 32, c.j0, c.j1, c.whole, c.cta0);
+                    sts128(dst + 48, c.cta1, c.starts, 0, 0);
+                    mbar_arrive(pfull(slot));
+                }
+                __syncwarp();
+                if (++slot == kPieces) { slot = 0; ph ^= 1u; }
+                if (f >= f_end) break;
+                f = line + c.j1;
+                if (f >= f_end) continue;            // announces the end
+                line += tiles;
+                if (++head == p.heads) {
+                    head = 0;
+                    if (++block == blocks) {
+                        block = 0;
+                        do {
+                            rq = load_request(p, ++r);
+                            blocks = blocks_of(p, rq);
+                        } while (blocks == 0 && r + 1 < p.requests);
+                    }
+                    block_tiles(p, rq, block, &lo_tile, &tiles);
+                }
+            }
+        } else if (warp < kMmaWarp + 2) {
+            // ---------------- MMA issuers, one warp per row tile ----------------
+            const int t = warp - kMmaWarp;
+            const uint32_t sa = tmem + kColS + kN * t, qa = tmem + kColQ + 64 * t, oa = tmem + kColO + 128 * t;
+            const uint32_t sf = sfull(t), wf = wfull(t);
+            int stage = 0;
+            uint32_t ph = 0;                         // decoded tiles, in the order K(j), V(j), K(j + 1), ...
+            uint32_t n_piece = 0, n_w = 0;
+            bool ok = true;
+            auto next_stage = [&]() { if (++stage == kStages) { stage = 0; ph ^= 1u; } };
+            auto mma_s = [&]() {
+                if (!warp_wait_inline(full(stage), ph, abort_flag, p.ws, kWaitMma)) return false;
                 tc_fence_after();
-                mma_s(t, ks);
-            }
-            if (!ok) break;
-            if (elect_one()) mma_commit(empty(ks));
-            __syncwarp();
-            advance();
-            for (int j = 0; j < n && ok; ++j, ++n_w) {
-                wait_stage();                        // V(j)
-                const int vs = stage;
-                advance();
-                for (int t = 0; t < 2 && ok; ++t) {
-                    ok = ok && warp_wait_inline(wfull(t), n_w & 1u, abort_flag, p.ws, kWaitMma);
-                    if (j == 0) ok = ok && warp_wait_inline(oempty(t), (n_piece & 1u) ^ 1u, abort_flag, p.ws, kWaitMma);
+                if (elect_one()) {
+                    const uint32_t kd = desc_lo(sbase + kStage0 + stage * kStageBytes, 16);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_f16_ta(sa, qa + 8 * k, desc_of(kd + (k / 4) * (kBlockBytes >> 4) + 2 * (k % 4)), kIdescS, k != 0);
+                    mma_commit(sf);
+                    mma_commit(empty(stage));
+                }
+                __syncwarp();
+                next_stage();
+                return true;
+            };
+            Reader rd{0, 0};
+            Piece c;
+            while (ok && read_piece(rd, c)) {
+                const int n = c.j1 - c.j0;
+                ok = warp_wait_inline(qfull(t), n_piece & 1u, abort_flag, p.ws, kWaitMma) && mma_s();
+                for (int j = 0; j < n && ok; ++j, ++n_w) {
+                    ok = warp_wait_inline(full(stage), ph, abort_flag, p.ws, kWaitMma) &&           // V(j)
+                         warp_wait_inline(wf, n_w & 1u, abort_flag, p.ws, kWaitMma) &&
+                         (j > 0 || warp_wait_inline(oempty(t), (n_piece & 1u) ^ 1u, abort_flag, p.ws, kWaitMma));
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint32_t vb = sbase + kStage0 + vs * kStageBytes;
+                        const uint32_t vd = desc_lo(sbase + kStage0 + stage * kStageBytes, kBlockBytes);
 #pragma unroll
                         for (int k = 0; k < kN / 16; ++k)
-                            mma_f16_ta(tmem + kColO + 128 * t, tmem + kColS + kN * t + 8 * k,
-                                       desc_values(vb, kBlockBytes) + 128 * k, kIdescO, j != 0 || k != 0);
-                        if (t == 1) mma_commit(empty(vs));
+                            mma_f16_ta(oa, sa + 8 * k, desc_of(vd + 128 * k), kIdescO, j != 0 || k != 0);
+                        mma_commit(empty(stage));
                         if (j + 1 == n) mma_commit(ofull(t));
                     }
                     __syncwarp();
-                    if (j + 1 < n) {
-                        // the next S of this row tile overwrites W behind the product that reads it
-                        if (t == 0) { wait_stage(); ks = stage; }
-                        if (!ok) break;
-                        tc_fence_after();
-                        mma_s(t, ks);
-                        if (t == 1) {
-                            if (elect_one()) mma_commit(empty(ks));
-                            __syncwarp();
-                            advance();
-                        }
-                    }
+                    next_stage();
+                    // the next S overwrites W behind the product that reads it
+                    if (j + 1 < n) ok = mma_s();
                 }
+                ++n_piece;
             }
-            ++n_piece;
-        } while (ok && walk.next(p));
         }
     } else if (warp < kTileWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
@@ -404,11 +426,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         int slot = 0;
         uint32_t rph = 0, n_s = 0, n_piece = 0;
         bool ok = true;
-        auto load_q = [&]() {
-            const Piece& c = walk.c;
-            const int row = c.block * kTileRows + row_in;
-            const bool live = row < c.rq.n * p.group;
-            const uint16_t* src = p.q + (int64_t)(c.rq.q0 + row / p.group) * p.q_stride +
+        auto load_q = [&](const Piece& c) {
+            const int row = c.row0 + row_in;
+            const bool live = row < c.n * p.group;
+            const uint16_t* src = p.q + (int64_t)(c.q0 + row / p.group) * p.q_stride +
                                   (int64_t)(c.head * p.group + row % p.group) * D;
 #pragma unroll
             for (int h = 0; h < D / 64; ++h) {
@@ -426,20 +447,23 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(qfull(t));
         };
-        load_q();
-        for (;;) {
-            const Piece c = walk.c;
-            const int row = c.block * kTileRows + row_in;
-            const int64_t pos = c.rq.kv - c.rq.n + row / p.group;
+        Reader rd{0, 0};
+        Piece c, c_next;
+        bool more = read_piece(rd, c_next);
+        if (more) load_q(c_next);
+        while (more) {
+            c = c_next;
+            const int row = c.row0 + row_in;
+            const int pos = c.kv - c.n + row / p.group;
             // keys this row sees: [klo, khi); those that all rows of its tile see need no mask
-            const int64_t khi = pos + 1 < c.rq.hi ? pos + 1 : c.rq.hi;
-            const int64_t klo = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;
-            const int64_t tile_first = c.rq.kv - c.rq.n + (c.block * kTileRows + t * 128) / p.group;
-            const int64_t tile_last = c.rq.kv - c.rq.n + (c.block * kTileRows + t * 128 + 127) / p.group;
-            const int64_t all_hi = tile_first + 1, all_lo = p.window > 0 ? tile_last - p.window + 1 : 0;
+            const int khi = pos + 1 < c.hi ? pos + 1 : c.hi;
+            const int klo = p.window > 0 && pos >= p.window ? pos - (int)p.window + 1 : 0;
+            const int tile_first = c.kv - c.n + (c.row0 + t * 128) / p.group;
+            const int tile_last = c.kv - c.n + (c.row0 + t * 128 + 127) / p.group;
+            const int all_hi = tile_first + 1, all_lo = p.window > 0 && tile_last >= p.window ? tile_last - (int)p.window + 1 : 0;
             float ref = kRefInit, sum = 0.0f;
             for (int j = c.j0; j < c.j1; ++j) {
-                const int64_t kb = (int64_t)(c.lo_tile + j) * kN;
+                const int kb = (c.lo_tile + j) * kN;
                 if (!warp_wait_inline(rfull(slot), rph, abort_flag, p.ws, kWaitSoftmax) ||
                     !warp_wait_inline(sfull(t), n_s & 1u, abort_flag, p.ws, kWaitSoftmax)) {
                     ok = false;
@@ -450,24 +474,29 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 const uint32_t rg = sbase + kSlot0 + slot * kSlotBytes;
                 float v[kN];
                 tmem_ld64(ts, v);
-                float top = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < kN; i += 4) {
                     const float4 k4 = lds_f4(rg + 4 * i), l4 = lds_f4(rg + 4 * kN + 4 * i);
-                    v[i] = fmaf(v[i], k4.x, l4.x);
-                    v[i + 1] = fmaf(v[i + 1], k4.y, l4.y);
-                    v[i + 2] = fmaf(v[i + 2], k4.z, l4.z);
-                    v[i + 3] = fmaf(v[i + 3], k4.w, l4.w);
+                    const float2 x = __ffma2_rn(make_float2(v[i], v[i + 1]), make_float2(k4.x, k4.y), make_float2(l4.x, l4.y));
+                    const float2 y = __ffma2_rn(make_float2(v[i + 2], v[i + 3]), make_float2(k4.z, k4.w), make_float2(l4.z, l4.w));
+                    v[i] = x.x; v[i + 1] = x.y; v[i + 2] = y.x; v[i + 3] = y.y;
                 }
                 const bool masked = kb + kN > all_hi || kb < all_lo;
                 if (masked) {
-                    const int a = klo > kb ? (int)(klo - kb < kN ? klo - kb : kN) : 0;
-                    const int b = khi > kb ? (int)(khi - kb < kN ? khi - kb : kN) : 0;
+                    // a hidden key's score is replaced, whatever its range holds
+                    const uint32_t a = klo > kb ? (uint32_t)(klo - kb < kN ? klo - kb : kN) : 0u;
+                    const uint32_t b = khi > kb ? (uint32_t)(khi - kb < kN ? khi - kb : kN) : 0u;
+                    const uint32_t seen = b > a ? b - a : 0u;
 #pragma unroll
-                    for (int i = 0; i < kN; ++i) v[i] = i >= a && i < b ? v[i] : -INFINITY;
+                    for (int i = 0; i < kN; ++i) v[i] = (uint32_t)i - a < seen ? v[i] : -INFINITY;
                 }
+                float top = -INFINITY, top2 = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < kN; ++i) top = fmaxf(top, v[i]);
+                for (int i = 0; i < kN; i += 4) {
+                    top = fmaxf(fmaxf(top, v[i]), v[i + 1]);
+                    top2 = fmaxf(fmaxf(top2, v[i + 2]), v[i + 3]);
+                }
+                top = fmaxf(top, top2);
                 if (__any_sync(0xffffffffu, top > ref + kRaise)) {
                     const float to_ref = fmaxf(ref, top);
                     const float f = exp2_approx(ref - to_ref);
@@ -485,27 +514,20 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                     }
                 }
                 uint32_t w[kN / 2];
-                float s0 = 0.0f, s1 = 0.0f;
+                float2 s0 = make_float2(0.0f, 0.0f), s1 = s0;
+                const float2 neg = make_float2(-ref, -ref);
 #pragma unroll
                 for (int i = 0; i < kN; i += 4) {
                     const float4 i4 = lds_f4(rg + 8 * kN + 4 * i);
-                    const float a = exp2_approx(v[i] - ref), b = exp2_approx(v[i + 1] - ref);
-                    const float c2 = exp2_approx(v[i + 2] - ref), d = exp2_approx(v[i + 3] - ref);
-                    if (!masked) {
-                        s0 = fmaf(a, i4.x, s0);
-                        s1 = fmaf(b, i4.y, s1);
-                        s0 = fmaf(c2, i4.z, s0);
-                        s1 = fmaf(d, i4.w, s1);
-                    } else {                         // a hidden key's range may be anything
-                        s0 = v[i] == -INFINITY ? s0 : fmaf(a, i4.x, s0);
-                        s1 = v[i + 1] == -INFINITY ? s1 : fmaf(b, i4.y, s1);
-                        s0 = v[i + 2] == -INFINITY ? s0 : fmaf(c2, i4.z, s0);
-                        s1 = v[i + 3] == -INFINITY ? s1 : fmaf(d, i4.w, s1);
-                    }
-                    w[i / 2] = pack2<true>(a, b);
-                    w[i / 2 + 1] = pack2<true>(c2, d);
+                    float2 x = __fadd2_rn(make_float2(v[i], v[i + 1]), neg), y = __fadd2_rn(make_float2(v[i + 2], v[i + 3]), neg);
+                    x = make_float2(exp2_approx(x.x), exp2_approx(x.y));
+                    y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                    s0 = __ffma2_rn(x, make_float2(i4.x, i4.y), s0);
+                    s1 = __ffma2_rn(y, make_float2(i4.z, i4.w), s1);
+                    w[i / 2] = pack2<true>(x.x, x.y);
+                    w[i / 2 + 1] = pack2<true>(y.x, y.y);
                 }
-                sum += s0 + s1;
+                sum += (s0.x + s0.y) + (s1.x + s1.y);
                 tmem_st_pairs(ts, w);
                 tmem_wait_st();
                 tc_fence_before();
@@ -518,15 +540,15 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             }
             if (!ok) break;
             // the piece's last S is read, so Q may be replaced and the next piece begin
-            const bool more = walk.next(p);
-            if (more) load_q();
+            more = read_piece(rd, c_next);
+            if (more) load_q(c_next);
             if (!warp_wait_inline(ofull(t), n_piece & 1u, abort_flag, p.ws, kWaitSoftmax)) break;
             ++n_piece;
             tc_fence_after();
-            const bool whole = c.j0 == 0 && c.j1 == c.tiles;
-            const bool live = row < c.rq.n * p.group;
-            float* part = p.parts + (size_t)(2 * blockIdx.x + (c.j0 == 0 ? 1 : 0)) * tile_slot_floats(D);
-            uint16_t* dst = p.out + ((int64_t)(c.rq.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group +
+            const bool whole = c.whole != 0;
+            const bool live = row < c.n * p.group;
+            float* part = p.parts + (size_t)(2 * blockIdx.x + c.starts) * tile_slot_floats(D);
+            uint16_t* dst = p.out + ((int64_t)(c.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group +
                                      row % p.group) * D;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll 1
@@ -556,8 +578,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             if (lane == 0) mbar_arrive(oempty(t));
             if (!whole) {
                 __stcg(reinterpret_cast<float2*>(part + (size_t)kTileRows * D) + row_in, make_float2(ref, sum));
-                const int64_t seg1 = c.line0 + c.tiles;
-                const int c0 = (int)(c.line0 / chunk), c1 = (int)((seg1 - 1) / chunk);
+                const int c0 = c.cta0, c1 = c.cta1;
                 __threadfence();
                 __syncwarp();
                 uint32_t last = 0;
@@ -589,7 +610,6 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                     }
                 }
             }
-            if (!more) break;
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsDecode));
@@ -604,48 +624,48 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         const int row_l = (lane & 7) + 8 * ((lane >> 3) / kChunks);
         const uint32_t lane4 = 4u * lane;
         auto task_row = [&](int i) { return (i * kDecWarps + dw) * kRowsPerWarp + row_l; };
-        // A tile whose loads are in flight.
+        // A tile whose pages are being looked up.
         struct Tile {
-            int64_t kb, hi;
-            int head;
+            int kb, hi, head;
             bool any;
             int32_t page[kTasks], page_r;
         };
-        Walk ahead = walk;                           // two tiles ahead of the decoding
-        int aj = ahead.c.j0;
+        Reader rd{0, 0};
+        Piece ahead;                                 // where the look-up is: two tiles before the decoding
+        ahead.j0 = ahead.j1 = 0;
         bool alive = true;
         const int shift = p.page_shift;
         auto fetch_pages = [&](Tile& x) {
+            if (alive && ahead.j0 == ahead.j1) alive = read_piece(rd, ahead);
             x.any = alive;
             if (!alive) return;
-            x.kb = (int64_t)(ahead.c.lo_tile + aj) * kN;
-            x.hi = ahead.c.rq.hi;
-            x.head = ahead.c.head;
-            const int32_t* table = p.block_table + ahead.c.r * p.table_width;
+            x.kb = (ahead.lo_tile + ahead.j0) * kN;
+            x.hi = ahead.hi;
+            x.head = ahead.head;
+            const int32_t* table = p.block_table + ahead.r * p.table_width;
 #pragma unroll
             for (int i = 0; i < kTasks; ++i) {
-                const int64_t key = x.kb + task_row(i);
+                const int key = x.kb + task_row(i);
                 x.page[i] = key < x.hi ? __ldg(table + (key >> shift)) : -1;
             }
-            const int64_t key = x.kb + dt;
+            const int key = x.kb + dt;
             x.page_r = dt < kN && key < x.hi ? __ldg(table + (key >> shift)) : -1;
-            if (++aj == ahead.c.j1) {
-                alive = ahead.next(p);
-                aj = ahead.c.j0;
-            }
+            ++ahead.j0;
         };
         struct Codes {
             uint4 k[kTasks], v[kTasks];
             uint16_t kr, vr;
             bool real;                               // this thread's key exists
+            bool any;
         };
         auto fetch_codes = [&](const Tile& x, Codes& c) {
+            c.any = x.any;
             if (!x.any) return;
 #pragma unroll
             for (int i = 0; i < kTasks; ++i) {
                 c.k[i] = c.v[i] = make_uint4(0, 0, 0, 0);
                 if (x.page[i] >= 0 && x.page[i] < p.pages) {
-                    const int64_t key = x.kb + task_row(i);
+                    const int key = x.kb + task_row(i);
                     const int64_t at = (((int64_t)x.page[i] * p.heads + x.head) * p.page_size + (key & (p.page_size - 1))) * (D / 2) + chunk_i * 16;
                     c.k[i] = __ldg(reinterpret_cast<const uint4*>(p.k_codes + at));
                     c.v[i] = __ldg(reinterpret_cast<const uint4*>(p.v_codes + at));
@@ -654,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             c.real = x.page_r >= 0 && x.page_r < p.pages;
             c.kr = c.vr = 0;
             if (c.real) {
-                const int64_t key = x.kb + dt;
+                const int key = x.kb + dt;
                 const int64_t at = ((int64_t)x.page_r * p.heads + x.head) * p.page_size + (key & (p.page_size - 1));
                 c.kr = __ldg(p.k_range + at);
                 c.vr = __ldg(p.v_range + at);
@@ -675,11 +695,13 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 const int row = task_row(i);
                 const uint32_t rb = base + (uint32_t)(chunk_i >> 1) * kBlockBytes + (uint32_t)row * 128;
                 const uint32_t x[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+                uint32_t y[16];                      // all lookups before the first store: they overlap
+#pragma unroll
+                for (int q = 0; q < 16; ++q) y[q] = lds_tab(prmt(x[q / 4], which, 0x7604u + 0x10u * (q % 4)));
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const uint32_t c16 = (uint32_t)((chunk_i & 1) * 4 + q) ^ (uint32_t)(row & 7);
-                    sts128(rb + c16 * 16, lds_tab(prmt(x[q], which, 0x7604u)), lds_tab(prmt(x[q], which, 0x7614u)),
-                           lds_tab(prmt(x[q], which, 0x7624u)), lds_tab(prmt(x[q], which, 0x7634u)));
+                    sts128(rb + c16 * 16, y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // visible to the MMA's reads
@@ -689,22 +711,23 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         };
         Tile pages;
         Codes cur, nxt;
-        fetch_pages(pages);
-        fetch_codes(pages, nxt);
-        fetch_pages(pages);
-        int64_t left = walk.f_end - walk.f;
-        for (; left > 0 && ok; --left) {
+        pages.any = nxt.any = false;
+        for (int n = -2; ok; ++n) {                  // tile n is decoded while n + 1 is read and n + 2 looked up
             cur = nxt;
             fetch_codes(pages, nxt);
             fetch_pages(pages);
+            if (n < 0) continue;
+            if (!cur.any) break;
             if (!warp_wait_inline(rempty(slot), rph ^ 1u, abort_flag, p.ws, kWaitDecode)) break;
             if (dt < kN) {
-                // a range of zero stands for zeros: any small one gives the same products
+                // A range of zero (or next to it) stands for zeros: any small one gives the same products.
+                // A range that is not finite reaches a row through its score alone, so
+                // that rows that do not see the key stay clear of it.
                 const float vr = to_float<F16>(cur.vr);
                 const uint32_t at = kSlot0 + slot * kSlotBytes + 4 * dt;
                 *reinterpret_cast<float*>(smem + at) = cur.real ? to_float<F16>(cur.kr) * p.scale_log2 : 0.0f;
-                *reinterpret_cast<float*>(smem + at + 4 * kN) = !cur.real ? -INFINITY : vr == 0.0f ? -60.0f : log2f(vr);
-                *reinterpret_cast<float*>(smem + at + 8 * kN) = !cur.real ? 0.0f : vr == 0.0f ? 0x1p60f : 1.0f / vr;
+                *reinterpret_cast<float*>(smem + at + 4 * kN) = !cur.real ? -INFINITY : vr < 0x1p-100f ? -60.0f : __log2f(vr);
+                *reinterpret_cast<float*>(smem + at + 8 * kN) = !cur.real ? 0.0f : vr < 0x1p-100f ? 0x1p60f : vr < INFINITY ? 1.0f / vr : 1.0f;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(rfull(slot));
@@ -716,9 +739,11 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
 
     // teardown: every MMA this CTA issued has completed before tensor memory is freed
     __syncthreads();
-    if (warp == kMmaWarp) {
+    if (warp == kMmaWarp || warp == kMmaWarp + 1) {
         if (elect_one()) mma_commit(drainb);
         __syncwarp();
+    }
+    if (warp == kMmaWarp) {
         warp_wait_inline(drainb, 0, abort_flag, p.ws, kWaitDrain, true);
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");

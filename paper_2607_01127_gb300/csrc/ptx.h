@@ -106,7 +106,10 @@ __device__ __forceinline__ bool warp_wait_inline(uint32_t bar, uint32_t parity, 
     uint32_t ok = 0;
     if ((threadIdx.x & 31) == 0)
         ok = mbar_try_wait(bar, parity) || wait_poll(bar, parity, abort_flag, ws, who, drain) ? 1u : 0u;
-    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+    // The other lanes skip the wait: nothing they read afterwards may be read
+    // before lane 0 is back, and a vote alone orders no memory.
+    __syncwarp();
+    return __any_sync(0xffffffffu, ok) != 0;         // uniform to the compiler, which a shuffle is not
 }
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
