@@ -158,9 +158,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     constexpr uint32_t kB3 = kB2 + 10 + 2 * kPieces;
     const uint32_t drainb = bar0 + 8u * kB3;
     const uint32_t tmem_slot = bar0 + 8u * (kB3 + 1);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + (tmem_slot + 8 - sbase));
-    int64_t* sched = reinterpret_cast<int64_t*>(smem + (tmem_slot + 16 - sbase));   // [24]
-    static_assert(8 * (kB3 + 2) + 16 + 8 * 24 <= 1024, "barrier block overflows");
+    int64_t* sched = reinterpret_cast<int64_t*>(smem + (tmem_slot + 8 - sbase));    // [24]
+    static_assert(8 * (kB3 + 2) + 8 + 8 * 24 <= 1024, "barrier block overflows");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
@@ -175,7 +174,6 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         }
         for (int s = 0; s < kPieces; ++s) { mbar_init(pfull(s), 1); mbar_init(pempty(s), 2 + kTileWarps + kDecWarps); }
         mbar_init(drainb, 2);
-        *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     for (int i = tid; i < 256 * 16; i += kThreads) {
@@ -273,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         uint32_t ph;
     };
     auto read_piece = [&](Reader& q, Piece& c) {
-        const bool ok = warp_wait_inline(pfull(q.slot), q.ph, abort_flag, p.ws, kWaitPlan);
+        const bool ok = warp_poll(pfull(q.slot), q.ph, p.ws, kWaitPlan);
         const uint32_t src = sbase + kPiece0 + q.slot * (uint32_t)sizeof(Piece);
         const uint4 a = lds128(src), b = lds128(src + 16), d = lds128(src + 32), e = lds128(src + 48);
         c.r = (int)a.x; c.q0 = (int)a.y; c.n = (int)a.z; c.kv = (int)a.w;
@@ -319,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             int slot = 0;
             uint32_t ph = 0;
             for (int64_t f = f0;;) {
-                if (!warp_wait_inline(pempty(slot), ph ^ 1u, abort_flag, p.ws, kWaitPlan)) break;
+                if (!warp_poll(pempty(slot), ph ^ 1u, p.ws, kWaitPlan)) break;
                 Piece c{};
                 if (f < f_end) {
                     const int64_t seg1 = line + tiles;
@@ -375,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             bool ok = true;
             auto next_stage = [&]() { if (++stage == kStages) { stage = 0; ph ^= 1u; } };
             auto mma_s = [&]() {
-                if (!warp_wait_inline(full(stage), ph, abort_flag, p.ws, kWaitMma)) return false;
+                if (!warp_poll(full(stage), ph, p.ws, kWaitMma)) return false;
                 tc_fence_after();
                 if (elect_one()) {
                     const uint32_t kd = desc_lo(sbase + kStage0 + stage * kStageBytes, 16);
@@ -393,11 +391,11 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             Piece c;
             while (ok && read_piece(rd, c)) {
                 const int n = c.j1 - c.j0;
-                ok = warp_wait_inline(qfull(t), n_piece & 1u, abort_flag, p.ws, kWaitMma) && mma_s();
+                ok = warp_poll(qfull(t), n_piece & 1u, p.ws, kWaitMma) && mma_s();
                 for (int j = 0; j < n && ok; ++j, ++n_w) {
-                    ok = warp_wait_inline(full(stage), ph, abort_flag, p.ws, kWaitMma) &&           // V(j)
-                         warp_wait_inline(wf, n_w & 1u, abort_flag, p.ws, kWaitMma) &&
-                         (j > 0 || warp_wait_inline(oempty(t), (n_piece & 1u) ^ 1u, abort_flag, p.ws, kWaitMma));
+                    ok = warp_poll(full(stage), ph, p.ws, kWaitMma) &&           // V(j)
+                         warp_poll(wf, n_w & 1u, p.ws, kWaitMma) &&
+                         (j > 0 || warp_poll(oempty(t), (n_piece & 1u) ^ 1u, p.ws, kWaitMma));
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
@@ -464,8 +462,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             float ref = kRefInit, sum = 0.0f;
             for (int j = c.j0; j < c.j1; ++j) {
                 const int kb = (c.lo_tile + j) * kN;
-                if (!warp_wait_inline(rfull(slot), rph, abort_flag, p.ws, kWaitSoftmax) ||
-                    !warp_wait_inline(sfull(t), n_s & 1u, abort_flag, p.ws, kWaitSoftmax)) {
+                if (!warp_poll(rfull(slot), rph, p.ws, kWaitSoftmax) ||
+                    !warp_poll(sfull(t), n_s & 1u, p.ws, kWaitSoftmax)) {
                     ok = false;
                     break;
                 }
@@ -542,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             // the piece's last S is read, so Q may be replaced and the next piece begin
             more = read_piece(rd, c_next);
             if (more) load_q(c_next);
-            if (!warp_wait_inline(ofull(t), n_piece & 1u, abort_flag, p.ws, kWaitSoftmax)) break;
+            if (!warp_poll(ofull(t), n_piece & 1u, p.ws, kWaitSoftmax)) break;
             ++n_piece;
             tc_fence_after();
             const bool whole = c.whole != 0;
@@ -685,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         bool ok = true;
         // which: this lane's copy of the keys' or of the values' entry, within a table row
         auto store = [&](uint32_t which, const uint4 (&codes)[kTasks]) {
-            if (!warp_wait_inline(empty(stage), ph ^ 1u, abort_flag, p.ws, kWaitDecode)) {
+            if (!warp_poll(empty(stage), ph ^ 1u, p.ws, kWaitDecode)) {
                 ok = false;
                 return;
             }
@@ -718,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             fetch_pages(pages);
             if (n < 0) continue;
             if (!cur.any) break;
-            if (!warp_wait_inline(rempty(slot), rph ^ 1u, abort_flag, p.ws, kWaitDecode)) break;
+            if (!warp_poll(rempty(slot), rph ^ 1u, p.ws, kWaitDecode)) break;
             if (dt < kN) {
                 // A range of zero (or next to it) stands for zeros: any small one gives the same products.
                 // A range that is not finite reaches a row through its score alone, so
@@ -744,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         __syncwarp();
     }
     if (warp == kMmaWarp) {
-        warp_wait_inline(drainb, 0, abort_flag, p.ws, kWaitDrain, true);
+        warp_poll(drainb, 0, p.ws, kWaitDrain);
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
