@@ -4,7 +4,7 @@
 // A segment is 256 query rows (tokens x query heads of a group) of one request
 // and kv head, as two tiles of 128 that share every decoded key and value; its
 // keys go by in tiles of 64.  Per key tile and row tile
-//   S = Q K^T          tcgen05.mma M = 128, N = 64,  A = Q from tensor memory
+//   S = Q K^T          tcgen05.mma M = 128, N = 64,  A = Q from tensor (half of it from shared) memory
 //   W = 2^(S * scale * range_k + log2 range_v - ref), rounded to fp16
 //   O += W V           tcgen05.mma M = 128, N = D,   A = W from tensor memory
 //   l += W / range_v
@@ -13,17 +13,19 @@
 // reference is raised (and O rescaled in tensor memory) only when a score
 // exceeds it by 2^8.
 //
-// What bounds it: with A in tensor memory a key tile costs 1024 cycles of MMA at
-// D = 128, and shared memory about as much (operands 512, decoded values written
-// 256, pair-table lookups 256, ranges), so the two row tiles alternate: while one
-// is in its softmax the tensor cores work for the other.  With Q in shared
-// memory its re-reads alone would take 512 cycles a key tile.
+// What bounds it: a key tile costs 1152 cycles of MMA at D = 128 and shared memory
+// about as much (operands, decoded values written, pair-table lookups, ranges), a
+// row tile's softmax somewhat more, so the two row tiles run independently and S of
+// the next key tile is computed while the softmax works on this one: W has a place
+// of its own.  That takes 64 columns more than tensor memory has, so half of Q (at
+// D = 128) is an operand in shared memory, whose re-reads slow those products by
+// half (48 cycles instead of 32).
 //
-// Tensor memory: S0 S1 (64 columns each; W overwrites the first half of its S)
-// | Q0 Q1 (64 each) | O0 O1 (128 each).
+// Tensor memory: S0 S1 (64 columns each) | W0 W1 (32) | Q0 Q1 (32: dimensions 0 .. 63)
+// | O0 O1 (128).
 // Warps: 0-3 and 4-7 softmax of row tile 0 and 1 (a thread per row; they also
 // load Q and write the results), 8-11 decode, 12 and 13 issue the MMAs of a row tile
-// each (one warp for both took longer to issue than the tensor cores to run).
+// each, 14 plans: it announces the pieces of segments that the CTA works on.
 //
 // Split: as in the small kernel the segments' key tiles form one line that the
 // CTAs cut evenly; the last warp to arrive joins the parts of its 32 rows.
@@ -58,17 +60,21 @@ constexpr int kPlanWarp = 14;
 constexpr int kThreads = 32 * 16;                // the last warp only completes the warpgroup
 // Registers per thread: 128 at launch; the softmax warps take what the others give back (2 x 160 + 96 + 96 = 4 x 128).
 constexpr int kRegsSoftmax = 160, kRegsDecode = 96, kRegsMma = 96;
-constexpr int kStages = 8;                       // decoded K / V tiles
+constexpr int kStagesK = 3, kStagesV = 4;        // decoded tiles
+constexpr int kPieceCost = 3;                    // a piece's start and end, in key tiles (~10k cycles)
 constexpr int kSlots = 4;                        // tiles' ranges
 constexpr int kMinTiles = 4;                     // key tiles per CTA, at least
 constexpr uint32_t kTabBytes = 256 * 256;        // pair tables: keys in the first, values in the second half of a row
 constexpr uint32_t kStageBytes = kN * 256;       // D = 128; D = 64 uses half
 constexpr uint32_t kSlotBytes = 3 * kN * 4;      // range_k * scale, log2 range_v, 1 / range_v
 constexpr int kPieces = 4;                       // pieces announced ahead
-constexpr uint32_t kStage0 = kTabBytes, kSlot0 = kStage0 + kStages * kStageBytes, kPiece0 = kSlot0 + kSlots * kSlotBytes;
+constexpr uint32_t kQBytes = 128 * 128;          // dimensions 64 .. 127 of a row tile's queries
+constexpr uint32_t kStageK0 = kTabBytes, kStageV0 = kStageK0 + kStagesK * kStageBytes;
+constexpr uint32_t kQ0 = kStageV0 + kStagesV * kStageBytes, kSlot0 = kQ0 + 2 * kQBytes;
+constexpr uint32_t kPiece0 = kSlot0 + kSlots * kSlotBytes;
 constexpr uint32_t kBar0 = kPiece0 + kPieces * sizeof(Piece);
 constexpr uint32_t kSmemBytes = kBar0 + 1024;
-constexpr uint32_t kColS = 0, kColQ = 128, kColO = 256, kTmemCols = 512;
+constexpr uint32_t kColS = 0, kColW = 128, kColQ = 192, kColO = 256, kTmemCols = 512;   // two of each, 64, 32, 32 and 128 columns
 enum : uint32_t { kWaitMma = 0x100, kWaitSoftmax = 0x101, kWaitDecode = 0x102, kWaitDrain = 0x103,
                   kWaitPlan = 0x104 };
 
@@ -142,20 +148,24 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
     const uint32_t bar0 = sbase + kBar0;
-    auto full = [&](int s) { return bar0 + 8u * s; };                       // decode -> MMA
-    auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
-    constexpr uint32_t kB1 = 2 * kStages;
+    auto kfull = [&](int s) { return bar0 + 8u * s; };                      // decode -> MMA: keys
+    auto kempty = [&](int s) { return bar0 + 8u * (kStagesK + s); };
+    constexpr uint32_t kBv = 2 * kStagesK;
+    auto vfull = [&](int s) { return bar0 + 8u * (kBv + s); };              // decode -> MMA: values
+    auto vempty = [&](int s) { return bar0 + 8u * (kBv + kStagesV + s); };
+    constexpr uint32_t kB1 = kBv + 2 * kStagesV;
     auto rfull = [&](int s) { return bar0 + 8u * (kB1 + s); };              // decode -> softmax: ranges
     auto rempty = [&](int s) { return bar0 + 8u * (kB1 + kSlots + s); };
     constexpr uint32_t kB2 = kB1 + 2 * kSlots;
     auto sfull = [&](int t) { return bar0 + 8u * (kB2 + t); };              // MMA -> softmax: S
-    auto wfull = [&](int t) { return bar0 + 8u * (kB2 + 2 + t); };          // softmax -> MMA: W
-    auto qfull = [&](int t) { return bar0 + 8u * (kB2 + 4 + t); };          // softmax -> MMA: Q of the next piece
-    auto ofull = [&](int t) { return bar0 + 8u * (kB2 + 6 + t); };          // MMA -> softmax: the piece's O
-    auto oempty = [&](int t) { return bar0 + 8u * (kB2 + 8 + t); };
-    auto pfull = [&](int s) { return bar0 + 8u * (kB2 + 10 + s); };         // planner -> all roles: a piece
-    auto pempty = [&](int s) { return bar0 + 8u * (kB2 + 10 + kPieces + s); };
-    constexpr uint32_t kB3 = kB2 + 10 + 2 * kPieces;
+    auto sempty = [&](int t) { return bar0 + 8u * (kB2 + 2 + t); };         // softmax -> MMA: S is in registers
+    auto wfull = [&](int t) { return bar0 + 8u * (kB2 + 4 + t); };          // softmax -> MMA: W
+    auto wempty = [&](int t) { return bar0 + 8u * (kB2 + 6 + t); };         // MMA -> softmax: W is used, O holds its products
+    auto qfull = [&](int t) { return bar0 + 8u * (kB2 + 8 + t); };          // softmax -> MMA: Q of the next piece
+    auto oempty = [&](int t) { return bar0 + 8u * (kB2 + 10 + t); };        // softmax -> MMA: the piece's O is read
+    auto pfull = [&](int s) { return bar0 + 8u * (kB2 + 12 + s); };         // planner -> all roles: a piece
+    auto pempty = [&](int s) { return bar0 + 8u * (kB2 + 12 + kPieces + s); };
+    constexpr uint32_t kB3 = kB2 + 12 + 2 * kPieces;
     const uint32_t drainb = bar0 + 8u * kB3;
     const uint32_t tmem_slot = bar0 + 8u * (kB3 + 1);
     int64_t* sched = reinterpret_cast<int64_t*>(smem + (tmem_slot + 8 - sbase));    // [24]
@@ -163,13 +173,15 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(full(s), kDecWarps); mbar_init(empty(s), 2); }
+        for (int s = 0; s < kStagesK; ++s) { mbar_init(kfull(s), kDecWarps); mbar_init(kempty(s), 2); }
+        for (int s = 0; s < kStagesV; ++s) { mbar_init(vfull(s), kDecWarps); mbar_init(vempty(s), 2); }
         for (int s = 0; s < kSlots; ++s) { mbar_init(rfull(s), kDecWarps); mbar_init(rempty(s), kTileWarps); }
         for (int t = 0; t < 2; ++t) {
             mbar_init(sfull(t), 1);
+            mbar_init(sempty(t), 4);
             mbar_init(wfull(t), 4);
+            mbar_init(wempty(t), 1);
             mbar_init(qfull(t), 4);
-            mbar_init(ofull(t), 1);
             mbar_init(oempty(t), 4);
         }
         for (int s = 0; s < kPieces; ++s) { mbar_init(pfull(s), 1); mbar_init(pempty(s), 2 + kTileWarps + kDecWarps); }
@@ -209,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             for (int b = lane; b < nb; b += 32) {
                 int lo, n;
                 block_tiles(p, x, b, &lo, &n);
-                sum += n;
+                sum += n + kPieceCost;
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -295,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             for (int b0 = 0; b0 < blocks; b0 += 32) {
                 int lo, n = 0;
                 if (b0 + lane < blocks) block_tiles(p, rq, b0 + lane, &lo, &n);
-                const int64_t w = (int64_t)n * p.heads;
+                const int64_t w = n > 0 ? (int64_t)(n + kPieceCost) * p.heads : 0;
                 int64_t incl = w;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -308,34 +320,16 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                     line += __shfl_sync(0xffffffffu, incl - w, src);
                     block = b0 + src;
                     block_tiles(p, rq, block, &lo_tile, &tiles);
-                    head = (int)((f0 - line) / tiles);
-                    line += (int64_t)head * tiles;
+                    head = (int)((f0 - line) / (tiles + kPieceCost));
+                    line += (int64_t)head * (tiles + kPieceCost);
                     break;
                 }
                 line += __shfl_sync(0xffffffffu, incl, 31);
             }
             int slot = 0;
             uint32_t ph = 0;
-            for (int64_t f = f0;;) {
-                if (!warp_poll(pempty(slot), ph ^ 1u, p.ws, kWaitPlan)) break;
-                Piece c{};
-                if (f < f_end) {
-                    const int64_t seg1 = line + tiles;
-                    c.r = (int)r;
-                    c.q0 = rq.q0;
-                    c.n = rq.n;
-                    c.kv = (int)rq.kv;
-                    c.hi = (int)rq.hi;
-                    c.row0 = block * kTileRows;
-                    c.head = head;
-                    c.lo_tile = lo_tile;
-                    c.j0 = (int)(f - line);
-                    c.j1 = (int)((f_end < seg1 ? f_end : seg1) - line);
-                    c.whole = c.j0 == 0 && c.j1 == tiles;
-                    c.cta0 = (int)(line / chunk);
-                    c.cta1 = (int)((seg1 - 1) / chunk);
-                    c.starts = c.j0 == 0;
-                }
+            auto announce = [&](const Piece& c) {
+                if (!warp_poll(pempty(slot), ph ^ 1u, p.ws, kWaitPlan)) return false;
                 if (lane == 0) {
                     const uint32_t dst = sbase + kPiece0 + slot * (uint32_t)sizeof(Piece);
                     sts128(dst, c.r, c.q0, c.n, c.kv);
@@ -346,11 +340,30 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 }
                 __syncwarp();
                 if (++slot == kPieces) { slot = 0; ph ^= 1u; }
-                if (f >= f_end) break;
-                f = line + c.j1;
-                if (f >= f_end) continue;            // announces the end
-                line += tiles;
-                if (++head == p.heads) {
+                return true;
+            };
+            // a segment takes kPieceCost places on the line, then one for each of its tiles
+            bool ok = true;
+            while (ok && line < f_end) {
+                const int64_t at = line + kPieceCost, end = at + tiles;
+                Piece c{};
+                c.r = (int)r;
+                c.q0 = rq.q0;
+                c.n = rq.n;
+                c.kv = (int)rq.kv;
+                c.hi = (int)rq.hi;
+                c.row0 = block * kTileRows;
+                c.head = head;
+                c.lo_tile = lo_tile;
+                c.j0 = f0 > at ? (int)(f0 - at) : 0;
+                c.j1 = f_end < end ? (int)(f_end - at) : tiles;
+                c.whole = c.j0 == 0 && c.j1 == tiles;
+                c.cta0 = (int)(at / chunk);
+                c.cta1 = (int)((end - 1) / chunk);
+                c.starts = c.j0 == 0;
+                if (c.j0 < c.j1) ok = announce(c);
+                line = end;
+                if (line < f_end && ++head == p.heads) {
                     head = 0;
                     if (++block == blocks) {
                         block = 0;
@@ -362,29 +375,36 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                     block_tiles(p, rq, block, &lo_tile, &tiles);
                 }
             }
+            if (ok) announce(Piece{});
         } else if (warp < kMmaWarp + 2) {
             // ---------------- MMA issuers, one warp per row tile ----------------
             const int t = warp - kMmaWarp;
-            const uint32_t sa = tmem + kColS + kN * t, qa = tmem + kColQ + 64 * t, oa = tmem + kColO + 128 * t;
-            const uint32_t sf = sfull(t), wf = wfull(t);
-            int stage = 0;
-            uint32_t ph = 0;                         // decoded tiles, in the order K(j), V(j), K(j + 1), ...
-            uint32_t n_piece = 0, n_w = 0;
+            const uint32_t sa = tmem + kColS + kN * t, wa = tmem + kColW + (kN / 2) * t;
+            const uint32_t qa = tmem + kColQ + 32 * t, oa = tmem + kColO + 128 * t;
+            const uint32_t qd = desc_lo(sbase + kQ0 + t * kQBytes, 16);
+            int ks = 0, vs = 0;
+            uint32_t kph = 0, vph = 0;
+            uint32_t n_piece = 0, n_s = 0, n_w = 0;
             bool ok = true;
-            auto next_stage = [&]() { if (++stage == kStages) { stage = 0; ph ^= 1u; } };
             auto mma_s = [&]() {
-                if (!warp_poll(full(stage), ph, p.ws, kWaitMma)) return false;
+                if (!warp_poll(kfull(ks), kph, p.ws, kWaitMma)) return false;
+                if (!warp_poll(sempty(t), (n_s & 1u) ^ 1u, p.ws, kWaitMma)) return false;
+                ++n_s;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint32_t kd = desc_lo(sbase + kStage0 + stage * kStageBytes, 16);
+                    const uint32_t kd = desc_lo(sbase + kStageK0 + ks * kStageBytes, 16);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        mma_f16_ta(sa, qa + 8 * k, desc_of(kd + (k / 4) * (kBlockBytes >> 4) + 2 * (k % 4)), kIdescS, k != 0);
-                    mma_commit(sf);
-                    mma_commit(empty(stage));
+                    for (int k = 0; k < 4; ++k) mma_f16_ta(sa, qa + 8 * k, desc_of(kd + 2 * k), kIdescS, k != 0);
+                    if constexpr (D == 128) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            mma_f16_ss(sa, desc_of(qd + 2 * k), desc_of(kd + (kBlockBytes >> 4) + 2 * k), kIdescS, 1);
+                    }
+                    mma_commit(sfull(t));
+                    mma_commit(kempty(ks));
                 }
                 __syncwarp();
-                next_stage();
+                if (++ks == kStagesK) { ks = 0; kph ^= 1u; }
                 return true;
             };
             Reader rd{0, 0};
@@ -393,23 +413,22 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 const int n = c.j1 - c.j0;
                 ok = warp_poll(qfull(t), n_piece & 1u, p.ws, kWaitMma) && mma_s();
                 for (int j = 0; j < n && ok; ++j, ++n_w) {
-                    ok = warp_poll(full(stage), ph, p.ws, kWaitMma) &&           // V(j)
-                         warp_poll(wf, n_w & 1u, p.ws, kWaitMma) &&
+                    // the next S while the softmax works on this one
+                    ok = (j + 1 == n || mma_s()) && warp_poll(vfull(vs), vph, p.ws, kWaitMma) &&
+                         warp_poll(wfull(t), n_w & 1u, p.ws, kWaitMma) &&
                          (j > 0 || warp_poll(oempty(t), (n_piece & 1u) ^ 1u, p.ws, kWaitMma));
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint32_t vd = desc_lo(sbase + kStage0 + stage * kStageBytes, kBlockBytes);
+                        const uint32_t vd = desc_lo(sbase + kStageV0 + vs * kStageBytes, kBlockBytes);
 #pragma unroll
                         for (int k = 0; k < kN / 16; ++k)
-                            mma_f16_ta(oa, sa + 8 * k, desc_of(vd + 128 * k), kIdescO, j != 0 || k != 0);
-                        mma_commit(empty(stage));
-                        if (j + 1 == n) mma_commit(ofull(t));
+                            mma_f16_ta(oa, wa + 8 * k, desc_of(vd + 128 * k), kIdescO, j != 0 || k != 0);
+                        mma_commit(wempty(t));
+                        mma_commit(vempty(vs));
                     }
                     __syncwarp();
-                    next_stage();
-                    // the next S overwrites W behind the product that reads it
-                    if (j + 1 < n) ok = mma_s();
+                    if (++vs == kStagesV) { vs = 0; vph ^= 1u; }
                 }
                 ++n_piece;
             }
@@ -420,25 +439,34 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         const int t = warp >> 2;                     // row tile
         const int row_in = t * 128 + (warp & 3) * 32 + lane;
         const uint32_t tq = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t ts = tq + kColS + kN * t, to = tq + kColO + 128 * t;
+        const uint32_t ts = tq + kColS + kN * t, tw = tq + kColW + (kN / 2) * t, to = tq + kColO + 128 * t;
         int slot = 0;
-        uint32_t rph = 0, n_s = 0, n_piece = 0;
+        uint32_t rph = 0, n_s = 0;
         bool ok = true;
         auto load_q = [&](const Piece& c) {
             const int row = c.row0 + row_in;
             const bool live = row < c.n * p.group;
             const uint16_t* src = p.q + (int64_t)(c.q0 + row / p.group) * p.q_stride +
                                   (int64_t)(c.head * p.group + row % p.group) * D;
+            uint32_t x[32];
 #pragma unroll
-            for (int h = 0; h < D / 64; ++h) {
-                uint32_t x[32];
+            for (int i = 0; i < 8; ++i) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (live) v = __ldg(reinterpret_cast<const uint4*>(src) + i);
+                x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+            }
+            tmem_st_pairs(tq + kColQ + 32 * t, x);
+            if constexpr (D == 128) {
+                // the upper half goes to shared memory: 128-byte rows, swizzled
+                const int m = (warp & 3) * 32 + lane;
+                const uint32_t rb = sbase + kQ0 + t * kQBytes + m * 128;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     uint4 v = make_uint4(0, 0, 0, 0);
-                    if (live) v = __ldg(reinterpret_cast<const uint4*>(src + 64 * h) + i);
-                    x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+                    if (live) v = __ldg(reinterpret_cast<const uint4*>(src + 64) + i);
+                    sts128(rb + 16 * (i ^ (m & 7)), v.x, v.y, v.z, v.w);
                 }
-                tmem_st_pairs(tq + kColQ + 64 * t + 32 * h, x);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
             tmem_wait_st();
             tc_fence_before();
@@ -472,6 +500,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 const uint32_t rg = sbase + kSlot0 + slot * kSlotBytes;
                 float v[kN];
                 tmem_ld64(ts, v);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sempty(t));
 #pragma unroll
                 for (int i = 0; i < kN; i += 4) {
                     const float4 k4 = lds_f4(rg + 4 * i), l4 = lds_f4(rg + 4 * kN + 4 * i);
@@ -495,6 +526,12 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                     top2 = fmaxf(fmaxf(top2, v[i + 2]), v[i + 3]);
                 }
                 top = fmaxf(top, top2);
+                // the products with the previous W are in O, and its place is free
+                if (!warp_poll(wempty(t), n_s & 1u, p.ws, kWaitSoftmax)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
                 if (__any_sync(0xffffffffu, top > ref + kRaise)) {
                     const float to_ref = fmaxf(ref, top);
                     const float f = exp2_approx(ref - to_ref);
@@ -526,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                     w[i / 2 + 1] = pack2<true>(y.x, y.y);
                 }
                 sum += (s0.x + s0.y) + (s1.x + s1.y);
-                tmem_st_pairs(ts, w);
+                tmem_st_pairs(tw, w);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -540,8 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             // the piece's last S is read, so Q may be replaced and the next piece begin
             more = read_piece(rd, c_next);
             if (more) load_q(c_next);
-            if (!warp_poll(ofull(t), n_piece & 1u, p.ws, kWaitSoftmax)) break;
-            ++n_piece;
+            if (!warp_poll(wempty(t), (n_s & 1u) ^ 1u, p.ws, kWaitSoftmax)) break;
             tc_fence_after();
             const bool whole = c.whole != 0;
             const bool live = row < c.n * p.group;
@@ -584,27 +620,41 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 if (__shfl_sync(0xffffffffu, last, 0)) {
                     __threadfence();
                     auto part_of = [&](int x) { return p.parts + (size_t)(2 * x + (x == c0 ? 1 : 0)) * tile_slot_floats(D); };
-                    float m = kRefInit;
-                    for (int x = c0; x <= c1; ++x)
-                        m = fmaxf(m, __ldcg(reinterpret_cast<const float2*>(part_of(x) + (size_t)kTileRows * D) + row_in).x);
-                    float l = 0.0f;
+                    auto stat_of = [&](int x) { return __ldcg(reinterpret_cast<const float2*>(part_of(x) + (size_t)kTileRows * D) + row_in); };
+                    float m = kRefInit, l = 0.0f;
+                    for (int x = c0; x <= c1; ++x) m = fmaxf(m, stat_of(x).x);
                     for (int x = c0; x <= c1; ++x) {
-                        const float2 st = __ldcg(reinterpret_cast<const float2*>(part_of(x) + (size_t)kTileRows * D) + row_in);
+                        const float2 st = stat_of(x);
                         l += st.y * exp2_approx(st.x - m);
                     }
                     const float li = l == 0.0f ? 0.0f : 1.0f / l;
-                    for (int d = 0; d < D && live; d += 8) {
-                        float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    // a row's dimensions across the lanes, so that the parts are read in whole lines
+                    constexpr int kLanes = D / 4, kPer = 32 / kLanes;
+                    const int64_t off = live ? (int64_t)(dst - p.out) : -1;
+                    const int d = (lane % kLanes) * 4;
+#pragma unroll 1
+                    for (int i0 = 0; i0 < 32; i0 += 8 * kPer) {
+                        float4 y[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) y[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                         for (int x = c0; x <= c1; ++x) {
-                            const float* src = part_of(x);
-                            const float k = exp2_approx(__ldcg(reinterpret_cast<const float2*>(src + (size_t)kTileRows * D) + row_in).x - m) * li;
-                            const float4 a = __ldcg(reinterpret_cast<const float4*>(src + (size_t)row_in * D + d));
-                            const float4 b = __ldcg(reinterpret_cast<const float4*>(src + (size_t)row_in * D + d) + 1);
-                            y[0] += a.x * k; y[1] += a.y * k; y[2] += a.z * k; y[3] += a.w * k;
-                            y[4] += b.x * k; y[5] += b.y * k; y[6] += b.z * k; y[7] += b.w * k;
+                            const float k = exp2_approx(stat_of(x).x - m) * li;
+                            const float* src = part_of(x) + (size_t)(row_in - lane + i0 + lane / kLanes) * D + d;
+                            float4 a[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) a[i] = __ldcg(reinterpret_cast<const float4*>(src + i * kPer * D));
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float f = __shfl_sync(0xffffffffu, k, i0 + i * kPer + lane / kLanes);
+                                y[i].x += a[i].x * f; y[i].y += a[i].y * f; y[i].z += a[i].z * f; y[i].w += a[i].w * f;
+                            }
                         }
-                        *reinterpret_cast<uint4*>(dst + d) = make_uint4(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]),
-                                                                       pack2<F16>(y[4], y[5]), pack2<F16>(y[6], y[7]));
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int64_t o = __shfl_sync(0xffffffffu, off, i0 + i * kPer + lane / kLanes);
+                            if (o >= 0)
+                                *reinterpret_cast<uint2*>(p.out + o + d) = make_uint2(pack2<F16>(y[i].x, y[i].y), pack2<F16>(y[i].z, y[i].w));
+                        }
                     }
                 }
             }
@@ -678,16 +728,11 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 c.vr = __ldg(p.v_range + at);
             }
         };
-        int stage = 0, slot = 0;
-        uint32_t ph = 0, rph = 0;
+        int ks = 0, vs = 0, slot = 0;
+        uint32_t kph = 0, vph = 0, rph = 0;
         bool ok = true;
         // which: this lane's copy of the keys' or of the values' entry, within a table row
-        auto store = [&](uint32_t which, const uint4 (&codes)[kTasks]) {
-            if (!warp_poll(empty(stage), ph ^ 1u, p.ws, kWaitDecode)) {
-                ok = false;
-                return;
-            }
-            const uint32_t base = sbase + kStage0 + stage * kStageBytes;
+        auto store = [&](uint32_t which, uint32_t base, const uint4 (&codes)[kTasks]) {
 #pragma unroll
             for (int i = 0; i < kTasks; ++i) {
                 const int row = task_row(i);
@@ -704,8 +749,6 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // visible to the MMA's reads
             __syncwarp();
-            if (lane == 0) mbar_arrive(full(stage));
-            if (++stage == kStages) { stage = 0; ph ^= 1u; }
         };
         Tile pages;
         Codes cur, nxt;
@@ -730,8 +773,16 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(rfull(slot));
             if (++slot == kSlots) { slot = 0; rph ^= 1u; }
-            store(lane4, cur.k);
-            if (ok) store(lane4 + 128u, cur.v);
+            ok = warp_poll(kempty(ks), kph ^ 1u, p.ws, kWaitDecode);
+            if (!ok) break;
+            store(lane4, sbase + kStageK0 + ks * kStageBytes, cur.k);
+            if (lane == 0) mbar_arrive(kfull(ks));
+            if (++ks == kStagesK) { ks = 0; kph ^= 1u; }
+            ok = warp_poll(vempty(vs), vph ^ 1u, p.ws, kWaitDecode);
+            if (!ok) break;
+            store(lane4 + 128u, sbase + kStageV0 + vs * kStageBytes, cur.v);
+            if (lane == 0) mbar_arrive(vfull(vs));
+            if (++vs == kStagesV) { vs = 0; vph ^= 1u; }
         }
     }
 
