@@ -45,11 +45,25 @@
 namespace logq {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
 constexpr int kStep = 16;                    // keys per warp step
-constexpr int kMinChunk = kWarps;            // steps per CTA, at least
+constexpr int kMinChunk = 20;                // places of the line per CTA, at least
+constexpr int kPieceCost = 12;               // joining a piece's warps, in steps (~1.3 us)
 constexpr uint32_t kTabBytes = 256 * 256;
+
+// Launch shapes by columns (8 NT): a batch-1 group of up to 8 query heads leaves
+// room for two CTAs an SM; more columns need the registers (O and Q of NT tiles).
+template <int NT>
+constexpr int warps_of = NT == 2 ? 12 : 8;
+template <int NT>
+constexpr int ctas_per_sm = NT == 1 ? 2 : 1;
+
+// The warps' O of 8 columns, or the statistics of a segment's parts (at most one a CTA).
+template <int D, int NT>
+__host__ __device__ constexpr size_t merge_bytes()
+{
+    const size_t o = (size_t)warps_of<NT> * 8 * (D + 4) * 4, parts = (size_t)kMaxCtas * 8 * NT * 8;
+    return o > parts ? o : parts;
+}
 
 template <uint32_t OFF>
 __device__ __forceinline__ uint32_t lds_tab(uint32_t off)
@@ -81,14 +95,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v)
     return r;
 }
 
-// floor(log2 r) of a range, kept within what the scaled weights and their sums can take.
-__device__ __forceinline__ float range_exponent(float r)
-{
-    int e = (int)((__float_as_uint(r) >> 23) & 0xffu) - 127;
-    e = e < -24 ? -24 : e > 100 ? 100 : e;
-    return (float)e;
-}
-
 // One request's share of the line of steps.
 struct Share : Request {
     int32_t lo_step;         // first step any of its tokens sees
@@ -100,28 +106,20 @@ __device__ __forceinline__ Share load_share(const KvAttendParams& p, int64_t r, 
 {
     Share q;
     static_cast<Request&>(q) = load_request(p, r);
-    const int64_t first = q.kv - q.n;
-    int64_t lo = p.window > 0 ? first - p.window + 1 : 0;
-    lo = lo < 0 ? 0 : lo;
-    q.lo_step = (int32_t)(lo / kStep);
-    const int64_t st = (q.hi + kStep - 1) / kStep - q.lo_step;
-    q.steps = st < 1 ? 1 : (int32_t)st;
-    if (st < 1) q.lo_step = 0;               // no key is seen: one step, hidden whole, inside the table
-    const int64_t rows = (int64_t)q.n * p.group;
-    q.blocks = rows > p.tile_rows ? 0 : (int32_t)((rows + nc - 1) / nc);
+    const int first = (int)q.kv - q.n, window = (int)p.window;
+    const int lo = window > 0 && first >= window ? first - window + 1 : 0;
+    q.lo_step = lo / kStep;
+    q.steps = ((int)q.hi + kStep - 1) / kStep - q.lo_step;
+    if (q.steps < 1) q.lo_step = 0, q.steps = 1;         // no key is seen: one step, hidden whole, inside the table
+    const int rows = q.n * p.group;
+    q.blocks = rows > p.tile_rows ? 0 : (rows + nc - 1) / nc;
     return q;
 }
 
+// Places on the line: each segment has kPieceCost, then one for each of its steps.
 __device__ __forceinline__ int64_t weight_of(const KvAttendParams& p, const Share& q)
 {
-    return (int64_t)q.blocks * p.heads * q.steps;
-}
-
-__device__ __forceinline__ int64_t warp_sum(int64_t v)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+    return (int64_t)q.blocks * p.heads * (q.steps + kPieceCost);
 }
 
 // The codes and ranges of one step as one lane needs them.
@@ -146,36 +144,18 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p)
     }
 }
 
-template <int D>
-__device__ __forceinline__ void load_step(StepData<D>& s, const KvAttendParams& p, int head, int64_t kb, int32_t page,
-                                          int g, int t)
-{
-    s.bad = page < 0 || page >= p.pages;
-    const int64_t row = ((int64_t)(s.bad ? 0 : page) * p.heads + head) * p.page_size + (kb & (p.page_size - 1));
-    const uint8_t* kc = p.k_codes + (row + g) * (D / 2) + t * (D / 8);
-    load_words(s.k[0], kc);
-    load_words(s.k[1], kc + 8 * (D / 2));
-    const uint8_t* vc = p.v_codes + (row + 2 * t) * (D / 2) + g * (D / 16);
-    load_words(s.v[0], vc);
-    load_words(s.v[1], vc + D / 2);
-    load_words(s.v[2], vc + 8 * (D / 2));
-    load_words(s.v[3], vc + 9 * (D / 2));
-    s.kr[0] = __ldg(p.k_range + row + g);
-    s.kr[1] = __ldg(p.k_range + row + g + 8);
-    s.vr[0] = __ldg(p.v_range + row + g);
-    s.vr[1] = __ldg(p.v_range + row + g + 8);
-}
-
 template <int D, bool F16, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const __grid_constant__ KvAttendParams p)
+__global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_kernel(const __grid_constant__ KvAttendParams p)
 {
+    constexpr int kWarps = warps_of<NT>, kThreads = 32 * kWarps;
     constexpr int NC = 8 * NT;
     constexpr int kOStride = D + 4;                  // floats per column of the merge buffer
     extern __shared__ __align__(1024) uint8_t smem[];
-    // layout: pair table | merge buffer [warp][8 columns][D] | {reference, sum} [warp][NC] | scratch
+    // layout: pair table | merge buffer [warp][8 columns][D], or the parts' statistics | {reference, sum} [warp][NC] | scratch
     float* merge = reinterpret_cast<float*>(smem + kTabBytes);
-    float2* stat = reinterpret_cast<float2*>(merge + kWarps * 8 * kOStride);
-    int64_t* scratch = reinterpret_cast<int64_t*>(stat + kWarps * NC);      // [kWarps + 4]
+    float2* pstat = reinterpret_cast<float2*>(merge);
+    float2* stat = reinterpret_cast<float2*>(smem + kTabBytes + merge_bytes<D, NT>());
+    int64_t* scratch = reinterpret_cast<int64_t*>(stat + kWarps * NC);      // [kWarps + 8]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, t = lane & 3;
 
@@ -189,73 +169,131 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // this CTA's piece [f, f_end) of the line, and the request it starts in
-    int64_t total = 0;
-    for (int64_t r = tid; r < p.requests; r += kThreads) total += weight_of(p, load_share(p, r, NC));
-    total = warp_sum(total);
-    if (lane == 0) scratch[warp] = total;
-    __syncthreads();
-    total = 0;
+    // this CTA's piece [f0, f_end) of the line, and the request it starts in: one
+    // scan over the requests, and one more where they are more than the threads
+    int64_t total = 0, f0 = 0, f_end = 0, chunk = 0;
+    const bool one_pass = p.requests <= kThreads;
+    if (!one_pass) {
+        for (int64_t r = tid; r < p.requests; r += kThreads) total += weight_of(p, load_share(p, r, NC));
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) total += scratch[w];
-    int64_t chunk = (total + gridDim.x - 1) / gridDim.x;
-    chunk = chunk < kMinChunk ? kMinChunk : chunk;
-    int64_t f = (int64_t)blockIdx.x * chunk;
-    const int64_t f_end = f + chunk < total ? f + chunk : total;
-    if (f >= f_end) return;
-    {
-        int64_t before = 0;
-        for (int64_t base = 0; base < p.requests; base += kThreads) {
-            const int64_t r = base + tid;
-            const int64_t w = r < p.requests ? weight_of(p, load_share(p, r, NC)) : 0;
-            int64_t incl = w;
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        if (lane == 0) scratch[warp] = total;
+        __syncthreads();
+        total = 0;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += u;
-            }
-            __syncthreads();
-            if (lane == 31) scratch[warp] = incl;
-            __syncthreads();
-            int64_t all = 0;
+        for (int w = 0; w < kWarps; ++w) total += scratch[w];
+    }
+    int64_t before = 0;
+    for (int64_t base = 0; base < p.requests; base += kThreads) {
+        const int64_t r = base + tid;
+        Share q;
+        int64_t w = 0;
+        if (r < p.requests) {
+            q = load_share(p, r, NC);
+            w = weight_of(p, q);
+        }
+        int64_t incl = w;
 #pragma unroll
-            for (int x = 0; x < kWarps; ++x) {
-                if (x < warp) incl += scratch[x];
-                all += scratch[x];
-            }
-            const int64_t from = before + incl - w;
-            if (w > 0 && from <= f && f < from + w) {
-                scratch[kWarps] = r;
-                scratch[kWarps + 1] = from;
-            }
-            before += all;
-            if (f < before) break;               // the same for every thread
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += u;
         }
         __syncthreads();
+        if (lane == 31) scratch[warp] = incl;
+        __syncthreads();
+        int64_t all = 0;
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) {
+            if (x < warp) incl += scratch[x];
+            all += scratch[x];
+        }
+        if (base == 0) {
+            if (one_pass) total = all;
+            chunk = (total + gridDim.x - 1) / gridDim.x;
+            chunk = chunk < kMinChunk ? kMinChunk : chunk;
+            f0 = (int64_t)blockIdx.x * chunk;
+            f_end = f0 + chunk < total ? f0 + chunk : total;
+            if (f0 >= f_end) return;                 // the whole CTA
+        }
+        const int64_t from = before + incl - w;
+        if (w > 0 && from <= f0 && f0 < from + w) {
+            scratch[kWarps] = r;
+            scratch[kWarps + 1] = from;
+            scratch[kWarps + 2] = (int64_t)q.q0 << 32 | (uint32_t)q.n;
+            scratch[kWarps + 3] = q.kv << 32 | (uint32_t)q.hi;
+            scratch[kWarps + 4] = (int64_t)q.lo_step << 32 | (uint32_t)q.steps;
+            scratch[kWarps + 5] = q.blocks;
+        }
+        before += all;
+        if (f0 < before) break;                      // the same for every thread
     }
-    int64_t r = scratch[kWarps], line0 = scratch[kWarps + 1];
-    Share rq = load_share(p, r, NC);
+    __syncthreads();
+    int64_t r = scratch[kWarps], line = scratch[kWarps + 1];
+    Share rq;
+    rq.q0 = (int32_t)(scratch[kWarps + 2] >> 32);
+    rq.n = (int32_t)scratch[kWarps + 2];
+    rq.kv = scratch[kWarps + 3] >> 32;
+    rq.hi = (int32_t)scratch[kWarps + 3];
+    rq.lo_step = (int32_t)(scratch[kWarps + 4] >> 32);
+    rq.steps = (int32_t)scratch[kWarps + 4];
+    rq.blocks = (int32_t)scratch[kWarps + 5];
+    int head, block;
+    {
+        const int64_t seg = (f0 - line) / (rq.steps + kPieceCost);
+        line += seg * (rq.steps + kPieceCost);
+        head = (int)(seg / rq.blocks);
+        block = (int)(seg % rq.blocks);
+    }
 
     const uint32_t lane4 = 4u * lane;
-    uint32_t* counters = p.counters;
-    float* parts = p.parts;
+    // this lane's places in a step
+    const uint8_t* const kp = p.k_codes + g * (D / 2) + t * (D / 8);
+    const uint8_t* const vp = p.v_codes + 2 * t * (D / 2) + g * (D / 16);
+    const uint16_t* const krp = p.k_range + g;
+    const uint16_t* const vrp = p.v_range + g;
+    const int64_t page_rows = (int64_t)p.heads * p.page_size;
 
-    while (f < f_end) {
-        while (f >= line0 + weight_of(p, rq)) {      // next request that has queries
-            line0 += weight_of(p, rq);
-            rq = load_share(p, ++r, NC);
-        }
-        const int64_t seg = (f - line0) / rq.steps;
-        const int64_t seg0 = line0 + seg * rq.steps, seg1 = seg0 + rq.steps;
-        const int64_t end = f_end < seg1 ? f_end : seg1;
-        const int head = (int)(seg / rq.blocks), block = (int)(seg % rq.blocks);
-        const int sb = (int)(f - seg0), cnt = (int)(end - f);
+    for (; line < f_end; ) {
+        const int64_t at = line + kPieceCost, seg_end = at + rq.steps;
+        const int sb = f0 > at ? (int)(f0 - at) : 0;
+        const int se = f_end < seg_end ? (int)(f_end - at) : rq.steps;
+        if (sb < se) {
         const int row0 = block * NC;                     // first query row (token * group + head in group)
         const int rows = rq.n * p.group - row0 < NC ? rq.n * p.group - row0 : NC;
-        const int64_t first_pos = rq.kv - rq.n + row0 / p.group;
-        const int64_t last_pos = rq.kv - rq.n + (row0 + rows - 1) / p.group;
+        const int kv = (int)rq.kv, hi = (int)rq.hi, window = (int)p.window;
+        const int first_pos = kv - rq.n + row0 / p.group;
+        const int last_pos = kv - rq.n + (row0 + rows - 1) / p.group;
 
         // ---------------- this warp's steps ----------------
+        const int cnt = se - sb;
+        const int s0 = sb + (int)((int64_t)cnt * warp / kWarps), s1 = sb + (int)((int64_t)cnt * (warp + 1) / kWarps);
+        const int32_t* table = p.block_table + r * p.table_width;
+        const int head_row = head * p.page_size;
+        auto page_of = [&](int s) { return __ldg(table + (((rq.lo_step + (s < s1 ? s : s1 - 1)) * kStep) >> p.page_shift)); };
+        int32_t page_next = 0;
+        auto load_step = [&](StepData<D>& d, int s) {
+            d.bad = (uint32_t)page_next >= (uint32_t)p.pages;
+            const int64_t row = (d.bad ? 0 : page_next * page_rows) + (head_row + (((rq.lo_step + s) * kStep) & (p.page_size - 1)));
+            const uint8_t* kc = kp + row * (D / 2);
+            load_words(d.k[0], kc);
+            load_words(d.k[1], kc + 8 * (D / 2));
+            const uint8_t* vc = vp + row * (D / 2);
+            load_words(d.v[0], vc);
+            load_words(d.v[1], vc + D / 2);
+            load_words(d.v[2], vc + 8 * (D / 2));
+            load_words(d.v[3], vc + 9 * (D / 2));
+            d.kr[0] = __ldg(krp + row);
+            d.kr[1] = __ldg(krp + row + 8);
+            d.vr[0] = __ldg(vrp + row);
+            d.vr[1] = __ldg(vrp + row + 8);
+            page_next = page_of(s + 1);
+        };
+        StepData<D> da, db;
+        if (s0 < s1) {
+            page_next = page_of(s0);
+            load_step(da, s0);
+        }
+
         uint32_t qf[NT][D / 8];                          // Q^T fragments: D / 4 dimensions from (D / 4) * t
         int khi[NT][2], klo[NT][2];                      // keys columns 2t, 2t + 1 see
 #pragma unroll
@@ -273,17 +311,15 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int col = nt * 8 + 2 * t + c;
-                const int64_t pos = rq.kv - rq.n + (row0 + col) / p.group;
+                const int pos = kv - rq.n + (row0 + col) / p.group;
                 const bool has = col < rows;             // other columns' results are dropped
-                int64_t hi = pos < rq.hi - 1 ? pos : rq.hi - 1;
-                int64_t lo = p.window > 0 && pos - p.window + 1 > 0 ? pos - p.window + 1 : 0;
-                khi[nt][c] = has ? (int)hi : INT_MAX;
-                klo[nt][c] = has ? (int)lo : 0;
+                khi[nt][c] = !has ? INT_MAX : pos < hi - 1 ? pos : hi - 1;
+                klo[nt][c] = has && window > 0 && pos >= window ? pos - window + 1 : 0;
             }
         }
         // keys that every column sees: no mask needed between these
-        const int64_t all_hi = first_pos < rq.hi - 1 ? first_pos : rq.hi - 1;
-        const int64_t all_lo = p.window > 0 ? last_pos - p.window + 1 : 0;
+        const int all_hi = first_pos < hi - 1 ? first_pos : hi - 1;
+        const int all_lo = window > 0 && last_pos >= window ? last_pos - window + 1 : 0;
 
         float o[NT][D / 16][4];
         float ref[NT][2], sum[NT][2];
@@ -297,27 +333,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
             for (int c = 0; c < 2; ++c) { ref[nt][c] = kRefInit; sum[nt][c] = 0.0f; }
         }
 
-        const int s0 = sb + (int)((int64_t)cnt * warp / kWarps), s1 = sb + (int)((int64_t)cnt * (warp + 1) / kWarps);
-        const int32_t* table = p.block_table + r * p.table_width;
-        auto key_of = [&](int s) { return (int64_t)(rq.lo_step + s) * kStep; };
-        auto page_of = [&](int s) {
-            const int64_t kb = key_of(s < s1 ? s : s1 - 1);
-            return __ldg(table + (kb >> p.page_shift));
-        };
-        StepData<D> next;
-        int32_t page_next = 0;
-        if (s0 < s1) {
-            load_step<D>(next, p, head, key_of(s0), page_of(s0), g, t);
-            page_next = page_of(s0 + 1);
-        }
-        for (int s = s0; s < s1; ++s) {
-            const StepData<D> cur = next;
-            if (s + 1 < s1) {
-                load_step<D>(next, p, head, key_of(s + 1), page_next, g, t);
-                page_next = page_of(s + 2);
-            }
-            const int64_t kb = key_of(s);
-
+        auto compute = [&](const StepData<D>& cur, int s) {
+            const int kb = (rq.lo_step + s) * kStep;
             // S^T = K Q^T
             float acc[NT][4];
 #pragma unroll
@@ -341,49 +358,51 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
                 }
             }
 
-            // weights p = 2^(s - ref), and W = p * range_v in fp16
-            const float ks[2] = {to_float<F16>(cur.kr[0]) * p.scale_log2, to_float<F16>(cur.kr[1]) * p.scale_log2};
-            float vr[2] = {to_float<F16>(cur.vr[0]), to_float<F16>(cur.vr[1])};
-            float ex[2] = {range_exponent(vr[0]), range_exponent(vr[1])};
+            // W = 2^(s + log2 range_v - ref), and the sum of W / range_v
+            float ks[2], lv[2], iv[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                ks[h] = to_float<F16>(cur.kr[h]) * p.scale_log2;
+                const float vr = scaled_range(to_float<F16>(cur.vr[h]));
+                lv[h] = __log2f(vr);
+                iv[h] = vr < INFINITY ? __fdividef(1.0f, vr) : 1.0f;
+            }
             const bool masked = cur.bad || kb + kStep - 1 > all_hi || kb < all_lo;
-            if (!masked) {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[nt][c] *= ks[c >> 1];
-            } else {
-                // a hidden key's range may be anything, NaN included: its score and
-                // its weight are replaced, not multiplied
+                for (int c = 0; c < 4; ++c) acc[nt][c] = fmaf(acc[nt][c], ks[c >> 1], lv[c >> 1]);
+            if (masked) {
+                // a hidden key's range may be anything, NaN included: its score is replaced
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const int64_t key = kb + g + 8 * (c >> 1);
-                        const bool seen = !cur.bad && key <= khi[nt][c & 1] && key >= klo[nt][c & 1];
-                        acc[nt][c] = seen ? acc[nt][c] * ks[c >> 1] : -INFINITY;
+                        const int key = kb + g + 8 * (c >> 1);
+                        if (cur.bad || key > khi[nt][c & 1] || key < klo[nt][c & 1]) acc[nt][c] = -INFINITY;
                     }
             }
             float high = -INFINITY;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) high = fmaxf(high, acc[nt][c] - ref[nt][c & 1] + ex[c >> 1]);
+                for (int c = 0; c < 2; ++c) high = fmaxf(high, fmaxf(acc[nt][c], acc[nt][c + 2]) - ref[nt][c]);
             if (__any_sync(0xffffffffu, high > kRaise)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float u = fmaxf(acc[nt][c] + ex[0], acc[nt][c + 2] + ex[1]);
+                        float u = fmaxf(acc[nt][c], acc[nt][c + 2]);
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) u = fmaxf(u, __shfl_xor_sync(0xffffffffu, u, x));
                         const float to = fmaxf(ref[nt][c], u);
-                        const float f0 = exp2_approx(ref[nt][c] - to);
+                        const float f = exp2_approx(ref[nt][c] - to);
                         ref[nt][c] = to;
-                        sum[nt][c] *= f0;
+                        sum[nt][c] *= f;
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
-                            o[nt][i][c] *= f0;
-                            o[nt][i][c + 2] *= f0;
+                            o[nt][i][c] *= f;
+                            o[nt][i][c + 2] *= f;
                         }
                     }
             }
@@ -393,10 +412,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
                 float w[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const float e = exp2_approx(acc[nt][c] - ref[nt][c & 1]);
-                    sum[nt][c & 1] += e;
-                    w[c] = e * vr[c >> 1];
-                    if (masked && acc[nt][c] == -INFINITY) w[c] = 0.0f;
+                    w[c] = exp2_approx(acc[nt][c] - ref[nt][c & 1]);
+                    sum[nt][c & 1] = fmaf(w[c], iv[c >> 1], sum[nt][c & 1]);
                 }
                 b[nt][0] = transpose8(pack2<true>(w[0], w[1]));
                 b[nt][1] = transpose8(pack2<true>(w[2], w[3]));
@@ -421,6 +438,13 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
                     for (int nt = 0; nt < NT; ++nt) mma16816<true>(o[nt][4 * w + j], a0, a1, a2, a3, b[nt][0], b[nt][1]);
                 }
             }
+        };
+        for (int s = s0; s < s1; s += 2) {
+            if (s + 1 < s1) load_step(db, s + 1);
+            compute(da, s);
+            if (s + 1 >= s1) break;
+            if (s + 2 < s1) load_step(da, s + 2);
+            compute(db, s + 1);
         }
 
         // ---------------- join the warps ----------------
@@ -433,24 +457,28 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
                 for (int x = 4; x < 32; x <<= 1) v += __shfl_xor_sync(0xffffffffu, v, x);
                 if (g == 0) stat[warp * NC + nt * 8 + 2 * t + c] = make_float2(ref[nt][c], v);
             }
-        const bool whole = f == seg0 && end == seg1;
-        // this piece's slot: the CTA's last segment when the segment starts here, else its first
-        const bool starts = f == seg0;
-        float* part = parts + (size_t)(2 * blockIdx.x + (starts ? 1 : 0)) * slot_floats(D);
+        const bool whole = sb == 0 && se == rq.steps;
+        // this piece's slot: the second of the CTA's two when the segment starts here
+        float* part = p.parts + (size_t)(2 * blockIdx.x + (sb == 0 ? 1 : 0)) * slot_floats(D);
+        auto write_out = [&](int col, int d, const float4& v, float l) {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const int row = row0 + col;
+            uint16_t* dst = p.out + ((int64_t)(rq.q0 + row / p.group) * (p.heads * p.group) + head * p.group + row % p.group) * D + d;
+            *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<F16>(v.x * inv, v.y * inv), pack2<F16>(v.z * inv, v.w * inv));
+        };
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                float* dst = merge + (warp * 8 + 2 * t + c) * kOStride + g * (D / 8);
+                float4* dst = reinterpret_cast<float4*>(merge + (warp * 8 + 2 * t + c) * kOStride + g * (D / 8));
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    dst[2 * i] = o[nt][i][c];
-                    dst[2 * i + 1] = o[nt][i][c + 2];
-                }
+                for (int i = 0; i < D / 16; i += 2)
+                    dst[i / 2] = make_float4(o[nt][i][c], o[nt][i][c + 2], o[nt][i + 1][c], o[nt][i + 1][c + 2]);
             }
             __syncthreads();
             for (int i = tid; i < 8 * (D / 4); i += kThreads) {
                 const int c = i / (D / 4), d = (i % (D / 4)) * 4, col = nt * 8 + c;
+                if (col >= rows) continue;
                 float m = kRefInit;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) m = fmaxf(m, stat[w * NC + col].x);
@@ -465,71 +493,71 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1) attend_kernel(const
                     v.x += x.x * k; v.y += x.y * k; v.z += x.z * k; v.w += x.w * k;
                 }
                 if (whole) {
-                    if (col < rows) {
-                        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                        const int row = row0 + col;
-                        uint16_t* dst = p.out + ((int64_t)(rq.q0 + row / p.group) * (p.heads * p.group) +
-                                                 head * p.group + row % p.group) * D + d;
-                        *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<F16>(v.x * inv, v.y * inv), pack2<F16>(v.z * inv, v.w * inv));
-                    }
+                    write_out(col, d, v, l);
                 } else {
                     __stcg(reinterpret_cast<float4*>(part + col * D + d), v);
-                    if (d == 0) {
-                        __stcg(part + kMaxCols * D + 2 * col, m);
-                        __stcg(part + kMaxCols * D + 2 * col + 1, l);
-                    }
+                    if (d == 0) __stcg(reinterpret_cast<float2*>(part + kMaxCols * D) + col, make_float2(m, l));
                 }
             }
             __syncthreads();
         }
         if (!whole) {
             // the last CTA of the segment to arrive joins the parts in key order
-            const int c0 = (int)(seg0 / chunk), c1 = (int)((seg1 - 1) / chunk);
+            const int c0 = (int)(at / chunk), n = (int)((seg_end - 1) / chunk) - c0 + 1;
             __threadfence();
             __syncthreads();
-            if (tid == 0) {
-                const uint32_t n = (uint32_t)(c1 - c0);
-                const bool last = atomicInc(&counters[c0], n) == n;        // wraps to 0
-                scratch[kWarps + 2] = last;
-            }
+            if (tid == 0)
+                scratch[kWarps + 6] = atomicInc(&p.counters[c0], (uint32_t)(n - 1)) == (uint32_t)(n - 1);    // wraps to 0
             __syncthreads();
-            const bool last = scratch[kWarps + 2] != 0;
-            if (last) {
+            if (scratch[kWarps + 6]) {
                 __threadfence();
-                for (int i = tid; i < NC * (D / 4); i += kThreads) {
+                auto part_of = [&](int x) { return p.parts + (size_t)(2 * (c0 + x) + (x == 0 ? 1 : 0)) * slot_floats(D); };
+                for (int i = tid; i < n * NC; i += kThreads)
+                    if (i % NC < rows) pstat[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i / NC) + kMaxCols * D) + i % NC);
+                __syncthreads();
+                for (int i = tid; i < rows * (D / 4); i += kThreads) {
                     const int col = i / (D / 4), d = (i % (D / 4)) * 4;
-                    if (col >= rows) continue;
                     float m = kRefInit;
-                    for (int c = c0; c <= c1; ++c) {
-                        const float* src = parts + (size_t)(2 * c + (c == c0 ? 1 : 0)) * slot_floats(D);
-                        m = fmaxf(m, __ldcg(src + kMaxCols * D + 2 * col));
-                    }
+                    for (int x = 0; x < n; ++x) m = fmaxf(m, pstat[x * NC + col].x);
                     float l = 0.0f;
                     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    for (int c = c0; c <= c1; ++c) {
-                        const float* src = parts + (size_t)(2 * c + (c == c0 ? 1 : 0)) * slot_floats(D);
-                        const float k = exp2_approx(__ldcg(src + kMaxCols * D + 2 * col) - m);
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(src + col * D + d));
-                        l += __ldcg(src + kMaxCols * D + 2 * col + 1) * k;
-                        v.x += x.x * k; v.y += x.y * k; v.z += x.z * k; v.w += x.w * k;
+                    for (int x0 = 0; x0 < n; x0 += 8) {
+                        float4 y[8];
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            y[x] = x0 + x < n ? __ldcg(reinterpret_cast<const float4*>(part_of(x0 + x) + col * D + d))
+                                              : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) {
+                            if (x0 + x >= n) break;
+                            const float2 st = pstat[(x0 + x) * NC + col];
+                            const float k = exp2_approx(st.x - m);
+                            l += st.y * k;
+                            v.x += y[x].x * k; v.y += y[x].y * k; v.z += y[x].z * k; v.w += y[x].w * k;
+                        }
                     }
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                    const int row = row0 + col;
-                    uint16_t* dst = p.out + ((int64_t)(rq.q0 + row / p.group) * (p.heads * p.group) + head * p.group +
-                                             row % p.group) * D + d;
-                    *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<F16>(v.x * inv, v.y * inv), pack2<F16>(v.z * inv, v.w * inv));
+                    write_out(col, d, v, l);
                 }
             }
             __syncthreads();
         }
-        f = end;
+        }
+        line = seg_end;
+        if (line < f_end && ++block == rq.blocks) {
+            block = 0;
+            if (++head == p.heads) {
+                head = 0;
+                do rq = load_share(p, ++r, NC);          // the next request that has queries here
+                while (rq.blocks == 0 && r + 1 < p.requests);
+            }
+        }
     }
 }
 
 template <int D, int NT>
 constexpr size_t smem_bytes()
 {
-    return kTabBytes + (size_t)kWarps * 8 * (D + 4) * 4 + (size_t)kWarps * 8 * NT * 8 + (kWarps + 4) * 8;
+    return kTabBytes + merge_bytes<D, NT>() + (size_t)warps_of<NT> * 8 * NT * 8 + (warps_of<NT> + 8) * 8;
 }
 
 template <int D, bool F16, int NT>
@@ -550,12 +578,11 @@ cudaError_t launch_attend(const KvAttendParams& p, cudaStream_t s)
         configured[dev] = true;
     }
     const int sms = sm_count() > 0 ? sm_count() : 148;
-    int grid = sms * (NT == 1 ? kMaxCtasPerSm : 1);
-    grid = grid < kMaxCtas ? grid : kMaxCtas;
+    const int grid = sms * ctas_per_sm<NT>;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3(grid < kMaxCtas ? grid : kMaxCtas);
+    cfg.blockDim = dim3(32 * warps_of<NT>);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = s;
     cudaLaunchAttribute at;
@@ -566,10 +593,15 @@ cudaError_t launch_attend(const KvAttendParams& p, cudaStream_t s)
     return cudaLaunchKernelEx(&cfg, attend_kernel<D, F16, NT>, p);
 }
 
+// The columns for up to max_rows query rows a kv head: as few passes over the
+// keys as 24 columns allow, and no wider than these passes need.
 template <int D, bool F16>
 cudaError_t launch_for(const KvAttendParams& p, int64_t max_rows, cudaStream_t s)
 {
-    return max_rows <= 8 ? launch_attend<D, F16, 1>(p, s) : launch_attend<D, F16, 2>(p, s);
+    const int64_t passes = (max_rows + kMaxCols - 1) / kMaxCols;
+    const int64_t cols = passes > 0 ? (max_rows + passes - 1) / passes : 1;
+    if (cols <= 8) return launch_attend<D, F16, 1>(p, s);
+    return cols <= 16 ? launch_attend<D, F16, 2>(p, s) : launch_attend<D, F16, 3>(p, s);
 }
 
 }  // namespace

@@ -77,8 +77,8 @@ cudaError_t launch_kv_append(const KvAppendParams& p, int head_dim, bool f16, cu
 // Workspace of the attention: record | arrival counters of the small and of the
 // large kernel | partial results of each, two slots per CTA.
 constexpr int kMaxCtasPerSm = 2;             // small kernel
-constexpr int kMaxCols = 16;                 // its query rows per segment, at most
-constexpr int kMaxCtas = 1024;
+constexpr int kMaxCols = 24;                 // its query rows per segment, at most
+constexpr int kMaxCtas = 320;                // CTAs of a launch, at most
 constexpr int kTileRows = 256;               // the large kernel's query rows per segment
 constexpr int kTileWarps = 8;                // its warps that hold query rows (32 each) and join parts by themselves
 constexpr size_t kCounterBytes = (size_t)kMaxCtas * (1 + kTileWarps) * sizeof(uint32_t);

@@ -40,6 +40,11 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     }
 }
 
+// The range that the weights are scaled by.  A range of zero stands for zeros: any
+// small one gives the same products, and 2^-60 keeps the sums exact; others are
+// kept above 2^-100, below which their reciprocals leave fp32.  NaN stays.
+__device__ __forceinline__ float scaled_range(float r) { return r == 0.0f ? 0x1p-60f : r < 0x1p-100f ? 0x1p-100f : r; }
+
 // A request as the attention kernels see it, its lengths made safe to index with.
 struct Request {
     int32_t q0, n;           // first token, tokens

@@ -61,7 +61,7 @@ constexpr int kThreads = 32 * 16;                // the last warp only completes
 // Registers per thread: 128 at launch; the softmax warps take what the others give back (2 x 160 + 96 + 96 = 4 x 128).
 constexpr int kRegsSoftmax = 160, kRegsDecode = 96, kRegsMma = 96;
 constexpr int kStagesK = 3, kStagesV = 4;        // decoded tiles
-constexpr int kPieceCost = 3;                    // a piece's start and end, in key tiles (~10k cycles)
+constexpr int kPieceCost = 4;                    // a piece's start and end, in key tiles (~11k cycles)
 constexpr int kSlots = 4;                        // tiles' ranges
 constexpr int kMinTiles = 4;                     // key tiles per CTA, at least
 constexpr uint32_t kTabBytes = 256 * 256;        // pair tables: keys in the first, values in the second half of a row
@@ -761,14 +761,13 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             if (!cur.any) break;
             if (!warp_poll(rempty(slot), rph ^ 1u, p.ws, kWaitDecode)) break;
             if (dt < kN) {
-                // A range of zero (or next to it) stands for zeros: any small one gives the same products.
                 // A range that is not finite reaches a row through its score alone, so
                 // that rows that do not see the key stay clear of it.
-                const float vr = to_float<F16>(cur.vr);
+                const float vr = scaled_range(to_float<F16>(cur.vr));
                 const uint32_t at = kSlot0 + slot * kSlotBytes + 4 * dt;
                 *reinterpret_cast<float*>(smem + at) = cur.real ? to_float<F16>(cur.kr) * p.scale_log2 : 0.0f;
-                *reinterpret_cast<float*>(smem + at + 4 * kN) = !cur.real ? -INFINITY : vr < 0x1p-100f ? -60.0f : __log2f(vr);
-                *reinterpret_cast<float*>(smem + at + 8 * kN) = !cur.real ? 0.0f : vr < 0x1p-100f ? 0x1p60f : vr < INFINITY ? 1.0f / vr : 1.0f;
+                *reinterpret_cast<float*>(smem + at + 4 * kN) = cur.real ? __log2f(vr) : -INFINITY;
+                *reinterpret_cast<float*>(smem + at + 8 * kN) = !cur.real ? 0.0f : vr < INFINITY ? __fdividef(1.0f, vr) : 1.0f;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(rfull(slot));
