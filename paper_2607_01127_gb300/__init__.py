@@ -415,13 +415,19 @@ def logq_device_sm_count() -> int:
 
 # ------------------------------------------------ paged 4-bit key/value cache ---
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _stream_int(stream, device):
+def _raw_stream(stream, index: int) -> int:
+    """The stream's handle; the current one of the device without making a Stream object (2 us)."""
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _check_int32(index: int, *tensors) -> None:
+    import torch
+    for x in tensors:
+        assert x.dtype is torch.int32 and x.is_contiguous() and x.get_device() == index, \
+            "contiguous int32 tensors on one CUDA device expected"
 
 
 class KVCache:
@@ -441,7 +447,7 @@ class KVCache:
         self.k_codes, self.k_range, self.v_codes, self.v_range = k_codes, k_range, v_codes, v_range
         self.k_cb, self.v_cb = k_cb, v_cb
         self.pages, self.heads, self.page_size, self.head_dim = pages, heads, page_size, 2 * half
-        self.dtype, self.device = k_range.dtype, k_codes.device
+        self.dtype, self.device, self._index = k_range.dtype, k_codes.device, k_codes.get_device()
         self._struct = KVCacheStruct(k_codes.data_ptr(), k_range.data_ptr(), v_codes.data_ptr(), v_range.data_ptr(),
                                      ctypes.pointer(k_cb), ctypes.pointer(v_cb), pages, page_size, heads, 2 * half,
                                      _dtype_code(k_range.dtype))
@@ -482,48 +488,53 @@ def logq_kv_plan(ctx_len, new_len, block_table, ring, ring_state, page_size: int
     returns (q_start, kv_len, positions, slots, ring_state).  ring_state is updated in place (with a
     workspace of logq_workspace_bytes(), new when none is given), or left as it was with inplace=False."""
     import torch
-    i32, dev = torch.int32, ctx_len.device
-    for x in (ctx_len, new_len, block_table, ring, ring_state):
-        assert x.dtype == i32 and x.is_contiguous() and x.device == dev and x.is_cuda, "int32 device tensors expected"
-    n = ctx_len.numel()
+    index, n = ctx_len.get_device(), ctx_len.numel()
+    assert index >= 0, "device tensors expected"
+    _check_int32(index, ctx_len, new_len, block_table, ring, ring_state)
     assert new_len.numel() == n and block_table.dim() == 2 and block_table.shape[0] == n and ring_state.numel() == 2
-    ints = torch.empty(2 * n + 3 + max_tokens, dtype=i32, device=dev)
-    q_start, kv_len, out, positions = ints.split([n + 1, n, 2, max_tokens])
-    slots = torch.empty(max_tokens, dtype=torch.int64, device=dev)
+    dev, i32, empty = ctx_len.device, torch.int32, torch.empty     # (a view costs more than an allocation)
+    q_start, kv_len = empty(n + 1, dtype=i32, device=dev), empty(n, dtype=i32, device=dev)
+    positions, slots = empty(max_tokens, dtype=i32, device=dev), empty(max_tokens, dtype=torch.int64, device=dev)
     if inplace:
         out = ring_state
         if workspace is None:
             workspace = new_workspace(dev)
+    else:
+        out = empty(2, dtype=i32, device=dev)
     st = _lib().logq_kv_plan(ctx_len.data_ptr(), new_len.data_ptr(), n, block_table.data_ptr(), block_table.shape[1],
                              page_size, ring.data_ptr(), ring.numel(), ring_state.data_ptr(), out.data_ptr(),
                              max_tokens, q_start.data_ptr(), kv_len.data_ptr(), positions.data_ptr(),
-                             slots.data_ptr(), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                             _stream_int(stream, dev))
+                             slots.data_ptr(), None if workspace is None else workspace.data_ptr(),
+                             0 if workspace is None else workspace.numel(), _raw_stream(stream, index))
     _check(st, "logq_kv_plan")
     return q_start, kv_len, positions, slots, out
 
 
 def _rows(x, heads, dim, cache, what):
     """Element stride between the tokens of x [tokens, heads, dim] whose heads are contiguous."""
-    assert x.dim() == 3 and x.shape[1] == heads and x.shape[2] == dim and x.dtype == cache.dtype, \
-        f"{what} must be [tokens, {heads}, {dim}] in the cache's dtype"
-    assert x.device == cache.device and x.stride(2) == 1 and x.stride(1) == dim, f"the heads of {what} must be contiguous"
-    return x.stride(0) if x.shape[0] > 1 else heads * dim
+    n, h, d = x.shape
+    assert h == heads and d == dim and x.dtype is cache.dtype, f"{what} must be [tokens, {heads}, {dim}] in the cache's dtype"
+    row, a, b = x.stride()
+    assert b == 1 and (a == dim or h == 1) and x.get_device() == cache._index, \
+        f"the heads of {what} must be contiguous, on the cache's device"
+    return row if n > 1 else heads * dim
 
 
 def logq_kv_append(cache: KVCache, k, v, slots, values: bool = False, stream=None):
     """Quantise keys and values [tokens, heads, head_dim] (token stride free) into the slots (int64).
     values=True returns (k_values, v_values): what the stored codes stand for."""
     import torch
-    ks, vs = _rows(k, cache.heads, cache.head_dim, cache, "k"), _rows(v, cache.heads, cache.head_dim, cache, "v")
-    n = k.shape[0]
-    assert v.shape[0] == n and slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() >= n
-    assert slots.device == cache.device
+    heads, dim, index = cache.heads, cache.head_dim, cache._index
+    ks, vs, n = _rows(k, heads, dim, cache, "k"), _rows(v, heads, dim, cache, "v"), k.shape[0]
+    assert v.shape[0] == n and slots.dtype is torch.int64 and slots.is_contiguous() and slots.numel() >= n \
+        and slots.get_device() == index, "slots: a contiguous int64 device tensor, one per token"
     kv = vv = None
     if values:
-        kv, vv = torch.empty(2, n, cache.heads, cache.head_dim, dtype=cache.dtype, device=cache.device).unbind(0)
-    st = _lib().logq_kv_append(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), n, _ptr(kv), _ptr(vv),
-                               _stream_int(stream, cache.device))
+        kv = torch.empty((n, heads, dim), dtype=cache.dtype, device=cache.device)
+        vv = torch.empty((n, heads, dim), dtype=cache.dtype, device=cache.device)
+    st = _lib().logq_kv_append(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), n,
+                               kv.data_ptr() if values else None, vv.data_ptr() if values else None,
+                               _raw_stream(stream, index))
     _check(st, "logq_kv_append")
     return (kv, vv) if values else None
 
@@ -534,22 +545,20 @@ def logq_kv_attention(cache: KVCache, q, q_start, kv_len, block_table, scale: fl
     its requests; scale defaults to head_dim ** -0.5, max_q (a bound of a request's tokens, for the
     choice of kernels) to tokens.  Returns out [tokens, q_heads, head_dim]."""
     import torch
-    tokens, hq = q.shape[0], q.shape[1]
-    qs = _rows(q, hq, cache.head_dim, cache, "q")
-    n = kv_len.numel()
-    for x in (q_start, kv_len, block_table):
-        assert x.dtype == torch.int32 and x.is_contiguous() and x.device == cache.device, "int32 device tensors expected"
+    tokens, hq, _ = q.shape
+    dim, index, n = cache.head_dim, cache._index, kv_len.numel()
+    qs = _rows(q, hq, dim, cache, "q")
+    _check_int32(index, q_start, kv_len, block_table)
     assert q_start.numel() == n + 1 and block_table.dim() == 2 and block_table.shape[0] == n
     if out is None:
-        out = torch.empty(tokens, hq, cache.head_dim, dtype=q.dtype, device=q.device)
+        out = torch.empty((tokens, hq, dim), dtype=cache.dtype, device=cache.device)
     else:
-        assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous() and out.device == q.device
+        assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
     if workspace is None:
-        workspace = new_kv_workspace(hq, cache.heads, cache.head_dim, cache.device)
+        workspace = new_kv_workspace(hq, cache.heads, dim, cache.device)
     st = _lib().logq_kv_attention(cache._ref, q.data_ptr(), qs, hq, tokens, q_start.data_ptr(), kv_len.data_ptr(), n,
-                                  block_table.data_ptr(), block_table.shape[1],
-                                  cache.head_dim ** -0.5 if scale is None else scale, window,
-                                  tokens if max_q is None else max_q, out.data_ptr(), workspace.data_ptr(),
-                                  workspace.numel(), _stream_int(stream, cache.device))
+                                  block_table.data_ptr(), block_table.shape[1], dim ** -0.5 if scale is None else scale,
+                                  window, tokens if max_q is None else max_q, out.data_ptr(), workspace.data_ptr(),
+                                  workspace.numel(), _raw_stream(stream, index))
     _check(st, "logq_kv_attention")
     return out

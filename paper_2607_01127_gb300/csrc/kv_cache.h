@@ -42,7 +42,7 @@ struct KvAppendParams {
     int64_t pages;
     int32_t page_size, page_shift, heads, pad_;
     float thresh[2][7];      // k, v: decision boundaries for range 1
-    uint16_t lvl16[2][16];   // k, v: levels in the cache's type
+    float level[2][8];       // k, v: positive levels of the cache's type
 };
 
 struct KvAttendParams {

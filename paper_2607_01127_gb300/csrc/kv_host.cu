@@ -41,11 +41,23 @@ logq_status check_cache(const logq_kv_cache* c)
     return LOGQ_OK;
 }
 
-uint16_t f16_of_bf16(uint16_t b)
+float f32_of_bf16(uint16_t b)
 {
     __nv_bfloat16 x;
     memcpy(&x, &b, 2);
-    const __half h = __float2half_rn(__bfloat162float(x));
+    return __bfloat162float(x);
+}
+
+float f32_of_f16(uint16_t b)
+{
+    __half x;
+    memcpy(&x, &b, 2);
+    return __half2float(x);
+}
+
+uint16_t f16_of_bf16(uint16_t b)
+{
+    const __half h = __float2half_rn(f32_of_bf16(b));
     uint16_t r;
     memcpy(&r, &h, 2);
     return r;
@@ -185,7 +197,7 @@ logq_status logq_kv_append(const logq_kv_cache* cache, const void* k, int64_t k_
     for (int i = 0; i < 2; ++i) {
         const logq_codebook* cb = i ? cache->v_cb : cache->k_cb;
         memcpy(p.thresh[i], cb->thresh, sizeof p.thresh[i]);
-        memcpy(p.lvl16[i], f16 ? cb->level_f16 : cb->level_bf16, sizeof p.lvl16[i]);
+        for (int m = 0; m < 8; ++m) p.level[i][m] = f16 ? f32_of_f16(cb->level_f16[m]) : f32_of_bf16(cb->level_bf16[m]);
     }
     return status_of(launch_kv_append(p, cache->head_dim, f16, static_cast<cudaStream_t>(stream)));
 }

@@ -103,6 +103,8 @@ def test_append(dtype, d, heads, page, tokens, extra, values):
         kv[0, 1, 3], kv[1, 2, 5], kv[0, 3, 0] = math.nan, math.inf, -math.inf
         kv[0, 4, :d] = torch.linspace(-1, 1, d).to(dtype)
         kv[1, 4, :d] = 2.0 ** -20                          # all at the range; subnormal in fp16
+    if tokens > 8:
+        kv[0, 6], kv[1, 7] = kv[0, 6] * 2.0 ** -14, kv[1, 7] * 2.0 ** -130   # subnormal in fp16, in bf16
     x = kv.cuda()
     k, v = (x[i, :, extra // 16 * 8:extra // 16 * 8 + heads * d].view(tokens, heads, d) for i in range(2))
     slots = torch.randperm(cache.pages * page, generator=gen)[:tokens].cuda()
