@@ -9,9 +9,10 @@
 //   O += W V           tcgen05.mma M = 128, N = D,   A = W from tensor memory
 //   l += W / range_v
 // with K and V decoded to 16-bit levels in shared memory and the ranges kept out
-// of the products, so that only W is rounded.  A row's thread owns the row: the
-// reference is raised (and O rescaled in tensor memory) only when a score
-// exceeds it by 2^8.
+// of the products, so that only W is rounded.  Each row's reference is raised (and
+// O rescaled in tensor memory) only when a score exceeds it by 2^8.  A lane reads S
+// as fragments of four rows x 16 keys, so that a key's three range values are loaded
+// once for four rows (a row per lane took 40% of shared memory's cycles for them).
 //
 // What bounds it: a key tile costs 1152 cycles of MMA at D = 128 and shared memory
 // about as much (operands, decoded values written, pair-table lookups, ranges), a
@@ -23,7 +24,7 @@
 //
 // Tensor memory: S0 S1 (64 columns each) | W0 W1 (32) | Q0 Q1 (32: dimensions 0 .. 63)
 // | O0 O1 (128).
-// Warps: 0-3 and 4-7 softmax of row tile 0 and 1 (a thread per row; they also
+// Warps: 0-3 and 4-7 softmax of row tile 0 and 1 (32 rows a warp; they also
 // load Q and write the results), 8-11 decode, 12 and 13 issue the MMAs of a row tile
 // each, 14 plans: it announces the pieces of segments that the CTA works on.
 //
@@ -66,7 +67,11 @@ constexpr int kSlots = 4;                        // tiles' ranges
 constexpr int kMinTiles = 4;                     // key tiles per CTA, at least
 constexpr uint32_t kTabBytes = 256 * 256;        // pair tables: keys in the first, values in the second half of a row
 constexpr uint32_t kStageBytes = kN * 256;       // D = 128; D = 64 uses half
-constexpr uint32_t kSlotBytes = 3 * kN * 4;      // range_k * scale, log2 range_v, 1 / range_v
+// A tile's range_k * scale, log2 range_v and 1 / range_v, each in the order of the
+// softmax's fragments: the 16 keys of lane % 4 = t from t * kRangeStride on (80
+// bytes apart, so that the four are read at once).
+constexpr int kRangeStride = 20;
+constexpr uint32_t kRangeBytes = 4 * kRangeStride * 4, kSlotBytes = 3 * kRangeBytes;
 constexpr int kPieces = 4;                       // pieces announced ahead
 constexpr uint32_t kQBytes = 128 * 128;          // dimensions 64 .. 127 of a row tile's queries
 constexpr uint32_t kStageK0 = kTabBytes, kStageV0 = kStageK0 + kStagesK * kStageBytes;
@@ -98,23 +103,44 @@ __device__ __forceinline__ void block_tiles(const KvAttendParams& p, const Reque
     *tiles = t1 > t0 ? t1 - t0 : 1;
 }
 
-// 64 consecutive columns of this warp's 32 lanes, complete on return.
-__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&r)[64])
+// 16 lanes x 64 columns as fragments: with g = lane / 4 and t = lane % 4, r[4 q]
+// and r[4 q + 1] are columns 8 q + 2 t and + 1 of row g, r[4 q + 2] and r[4 q + 3]
+// those of row g + 8.
+__device__ __forceinline__ void tmem_ld_frag(uint32_t taddr, float* r)
 {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
-        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
         : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
           "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
           "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
-          "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31]),
-          "=f"(r[32]), "=f"(r[33]), "=f"(r[34]), "=f"(r[35]), "=f"(r[36]), "=f"(r[37]), "=f"(r[38]), "=f"(r[39]),
-          "=f"(r[40]), "=f"(r[41]), "=f"(r[42]), "=f"(r[43]), "=f"(r[44]), "=f"(r[45]), "=f"(r[46]), "=f"(r[47]),
-          "=f"(r[48]), "=f"(r[49]), "=f"(r[50]), "=f"(r[51]), "=f"(r[52]), "=f"(r[53]), "=f"(r[54]), "=f"(r[55]),
-          "=f"(r[56]), "=f"(r[57]), "=f"(r[58]), "=f"(r[59]), "=f"(r[60]), "=f"(r[61]), "=f"(r[62]), "=f"(r[63])
+          "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
         : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_frag(uint32_t taddr, const float* r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+        ::"r"(taddr), "f"(r[0]), "f"(r[1]), "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]),
+          "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]), "f"(r[14]), "f"(r[15]),
+          "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]),
+          "f"(r[24]), "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31])
+        : "memory");
+}
+// All loads issued before are complete; the registers are tied to it so that nothing uses them earlier.
+__device__ __forceinline__ void tmem_wait_frag(float* r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(r[i]));
+}
+// 16 lanes x 32 columns of 16-bit pairs: r[2 q] is column 4 q + t of row g, r[2 q + 1] of row g + 8.
+__device__ __forceinline__ void tmem_st_pairs_frag(uint32_t taddr, const uint32_t* r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
 
@@ -435,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         }
     } else if (warp < kTileWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        // ---------------- softmax, one thread per query row ----------------
+        // ---------------- softmax, 32 query rows a warp ----------------
         const int t = warp >> 2;                     // row tile
         const int row_in = t * 128 + (warp & 3) * 32 + lane;
         const uint32_t tq = tmem + ((uint32_t)((warp & 3) * 32) << 16);
@@ -479,15 +505,22 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         if (more) load_q(c_next);
         while (more) {
             c = c_next;
-            const int row = c.row0 + row_in;
-            const int pos = c.kv - c.n + row / p.group;
-            // keys this row sees: [klo, khi); those that all rows of its tile see need no mask
-            const int khi = pos + 1 < c.hi ? pos + 1 : c.hi;
-            const int klo = p.window > 0 && pos >= p.window ? pos - (int)p.window + 1 : 0;
+            // the keys that this lane's four rows (16 h + 8 b + g) see: [klo, klo + seen); those
+            // that all rows of the tile see need no mask
+            int klo[4], khi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int pos = c.kv - c.n + (c.row0 + t * 128 + (warp & 3) * 32 + 8 * i + (lane >> 2)) / p.group;
+                khi[i] = pos + 1 < c.hi ? pos + 1 : c.hi;
+                klo[i] = p.window > 0 && pos >= p.window ? pos - (int)p.window + 1 : 0;
+            }
             const int tile_first = c.kv - c.n + (c.row0 + t * 128) / p.group;
             const int tile_last = c.kv - c.n + (c.row0 + t * 128 + 127) / p.group;
             const int all_hi = tile_first + 1, all_lo = p.window > 0 && tile_last >= p.window ? tile_last - (int)p.window + 1 : 0;
-            float ref = kRefInit, sum = 0.0f;
+            float ref[4];
+            float2 sum[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { ref[i] = kRefInit; sum[i] = make_float2(0.0f, 0.0f); }
             for (int j = c.j0; j < c.j1; ++j) {
                 const int kb = (c.lo_tile + j) * kN;
                 if (!warp_poll(rfull(slot), rph, p.ws, kWaitSoftmax) ||
@@ -497,73 +530,106 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 }
                 ++n_s;
                 tc_fence_after();
-                const uint32_t rg = sbase + kSlot0 + slot * kSlotBytes;
+                const uint32_t rg = sbase + kSlot0 + slot * kSlotBytes + (lane & 3) * (kRangeStride * 4);
+                // v[32 h + 4 q + 2 b + e]: row 16 h + 8 b + g, key 8 q + 2 (lane % 4) + e
                 float v[kN];
-                tmem_ld64(ts, v);
+                tmem_ld_frag(ts, v);
+                tmem_ld_frag(ts + (16u << 16), v + 32);
+                tmem_wait_frag(v);
+                tmem_wait_frag(v + 32);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(sempty(t));
 #pragma unroll
-                for (int i = 0; i < kN; i += 4) {
-                    const float4 k4 = lds_f4(rg + 4 * i), l4 = lds_f4(rg + 4 * kN + 4 * i);
-                    const float2 x = __ffma2_rn(make_float2(v[i], v[i + 1]), make_float2(k4.x, k4.y), make_float2(l4.x, l4.y));
-                    const float2 y = __ffma2_rn(make_float2(v[i + 2], v[i + 3]), make_float2(k4.z, k4.w), make_float2(l4.z, l4.w));
-                    v[i] = x.x; v[i + 1] = x.y; v[i + 2] = y.x; v[i + 3] = y.y;
+                for (int q = 0; q < 8; q += 2) {
+                    const float4 k4 = lds_f4(rg + 8 * q), l4 = lds_f4(rg + kRangeBytes + 8 * q);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {        // rows and the two q
+                        float* x = v + 32 * (i >> 2) + 4 * (q + (i & 1)) + (i & 2);
+                        const float2 k2 = i & 1 ? make_float2(k4.z, k4.w) : make_float2(k4.x, k4.y);
+                        const float2 l2 = i & 1 ? make_float2(l4.z, l4.w) : make_float2(l4.x, l4.y);
+                        const float2 y = __ffma2_rn(make_float2(x[0], x[1]), k2, l2);
+                        x[0] = y.x;
+                        x[1] = y.y;
+                    }
                 }
-                const bool masked = kb + kN > all_hi || kb < all_lo;
-                if (masked) {
+                if (kb + kN > all_hi || kb < all_lo) {
                     // a hidden key's score is replaced, whatever its range holds
-                    const uint32_t a = klo > kb ? (uint32_t)(klo - kb < kN ? klo - kb : kN) : 0u;
-                    const uint32_t b = khi > kb ? (uint32_t)(khi - kb < kN ? khi - kb : kN) : 0u;
-                    const uint32_t seen = b > a ? b - a : 0u;
 #pragma unroll
-                    for (int i = 0; i < kN; ++i) v[i] = (uint32_t)i - a < seen ? v[i] : -INFINITY;
-                }
-                float top = -INFINITY, top2 = -INFINITY;
+                    for (int i = 0; i < 4; ++i) {
+                        const int lo = klo[i] > kb ? (klo[i] - kb < kN ? klo[i] - kb : kN) : 0;
+                        const int hi = khi[i] > kb ? (khi[i] - kb < kN ? khi[i] - kb : kN) : 0;
+                        const uint32_t seen = hi > lo ? (uint32_t)(hi - lo) : 0u;
+                        const uint32_t from = (uint32_t)(lo - 2 * (lane & 3));
 #pragma unroll
-                for (int i = 0; i < kN; i += 4) {
-                    top = fmaxf(fmaxf(top, v[i]), v[i + 1]);
-                    top2 = fmaxf(fmaxf(top2, v[i + 2]), v[i + 3]);
+                        for (int q = 0; q < 8; ++q)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float& x = v[32 * (i >> 1) + 4 * q + 2 * (i & 1) + e];
+                                x = (uint32_t)(8 * q + e) - from < seen ? x : -INFINITY;
+                            }
+                    }
                 }
-                top = fmaxf(top, top2);
+                float top[4];
+                bool raise = false;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float* x = v + 32 * (i >> 1) + 2 * (i & 1);
+                    top[i] = fmaxf(x[0], x[1]);
+#pragma unroll
+                    for (int q = 1; q < 8; ++q) top[i] = fmaxf(fmaxf(top[i], x[4 * q]), x[4 * q + 1]);
+                    raise = raise || top[i] > ref[i] + kRaise;
+                }
                 // the products with the previous W are in O, and its place is free
                 if (!warp_poll(wempty(t), n_s & 1u, p.ws, kWaitSoftmax)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                if (__any_sync(0xffffffffu, top > ref + kRaise)) {
-                    const float to_ref = fmaxf(ref, top);
-                    const float f = exp2_approx(ref - to_ref);
-                    ref = to_ref;
-                    sum *= f;
+                if (__any_sync(0xffffffffu, raise)) {
+                    float f[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+                        top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+                        const float to_ref = fmaxf(ref[i], top[i]);
+                        f[i] = exp2_approx(ref[i] - to_ref);
+                        ref[i] = to_ref;
+                        sum[i].x *= f[i];
+                        sum[i].y *= f[i];
+                    }
                     if (j != c.j0) {                 // O holds the products of all earlier key tiles
 #pragma unroll 1
-                        for (int h = 0; h < D / 32; ++h) {
-                            uint32_t o[32];
-                            tmem_ld32(to + 32 * h, o);
+                        for (int h = 0; h < D / 32; ++h) {   // 64 columns of the lower, then of the upper 16 rows
+                            const uint32_t at = to + 64 * (h >> 1) + (uint32_t)((h & 1) * 16 << 16);
+                            float o[32];
+                            tmem_ld_frag(at, o);
+                            tmem_wait_frag(o);
+                            const float fa = h & 1 ? f[2] : f[0], fb = h & 1 ? f[3] : f[1];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st_pairs(to + 32 * h, o);
+                            for (int i = 0; i < 32; ++i) o[i] *= i & 2 ? fb : fa;
+                            tmem_st_frag(at, o);
                         }
                     }
                 }
-                uint32_t w[kN / 2];
-                float2 s0 = make_float2(0.0f, 0.0f), s1 = s0;
-                const float2 neg = make_float2(-ref, -ref);
+                uint32_t w[kN / 2];                  // w[16 h + 2 q + b]
+                const float2 neg[4] = {make_float2(-ref[0], -ref[0]), make_float2(-ref[1], -ref[1]),
+                                       make_float2(-ref[2], -ref[2]), make_float2(-ref[3], -ref[3])};
 #pragma unroll
-                for (int i = 0; i < kN; i += 4) {
-                    const float4 i4 = lds_f4(rg + 8 * kN + 4 * i);
-                    float2 x = __fadd2_rn(make_float2(v[i], v[i + 1]), neg), y = __fadd2_rn(make_float2(v[i + 2], v[i + 3]), neg);
-                    x = make_float2(exp2_approx(x.x), exp2_approx(x.y));
-                    y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
-                    s0 = __ffma2_rn(x, make_float2(i4.x, i4.y), s0);
-                    s1 = __ffma2_rn(y, make_float2(i4.z, i4.w), s1);
-                    w[i / 2] = pack2<true>(x.x, x.y);
-                    w[i / 2 + 1] = pack2<true>(y.x, y.y);
+                for (int q = 0; q < 8; q += 2) {
+                    const float4 i4 = lds_f4(rg + 2 * kRangeBytes + 8 * q);
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) {
+                        const int i = z >> 1, qq = q + (z & 1);
+                        const float* x = v + 32 * (i >> 1) + 4 * qq + 2 * (i & 1);
+                        float2 y = __fadd2_rn(make_float2(x[0], x[1]), neg[i]);
+                        y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                        sum[i] = __ffma2_rn(y, z & 1 ? make_float2(i4.z, i4.w) : make_float2(i4.x, i4.y), sum[i]);
+                        w[16 * (i >> 1) + 2 * qq + (i & 1)] = pack2<true>(y.x, y.y);
+                    }
                 }
-                sum += (s0.x + s0.y) + (s1.x + s1.y);
-                tmem_st_pairs(tw, w);
+                tmem_st_pairs_frag(tw, w);
+                tmem_st_pairs_frag(tw + (16u << 16), w + 16);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -579,12 +645,23 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             if (more) load_q(c_next);
             if (!warp_poll(wempty(t), (n_s & 1u) ^ 1u, p.ws, kWaitSoftmax)) break;
             tc_fence_after();
+            // from here a lane has the row of its number: fetch that row's sum and reference
+            const int row = c.row0 + row_in;
+            float row_ref = 0.0f, row_sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float l = sum[i].x + sum[i].y;
+                l += __shfl_xor_sync(0xffffffffu, l, 1);
+                l += __shfl_xor_sync(0xffffffffu, l, 2);
+                const float a = __shfl_sync(0xffffffffu, l, 4 * (lane & 7)), b = __shfl_sync(0xffffffffu, ref[i], 4 * (lane & 7));
+                if (lane >> 3 == i) row_sum = a, row_ref = b;
+            }
             const bool whole = c.whole != 0;
             const bool live = row < c.n * p.group;
             float* part = p.parts + (size_t)(2 * blockIdx.x + c.starts) * tile_slot_floats(D);
             uint16_t* dst = p.out + ((int64_t)(c.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group +
                                      row % p.group) * D;
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            const float inv = row_sum == 0.0f ? 0.0f : 1.0f / row_sum;
 #pragma unroll 1
             for (int h = 0; h < D / 32; ++h) {
                 uint32_t o[32];
@@ -611,7 +688,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             __syncwarp();
             if (lane == 0) mbar_arrive(oempty(t));
             if (!whole) {
-                __stcg(reinterpret_cast<float2*>(part + (size_t)kTileRows * D) + row_in, make_float2(ref, sum));
+                __stcg(reinterpret_cast<float2*>(part + (size_t)kTileRows * D) + row_in, make_float2(row_ref, row_sum));
                 const int c0 = c.cta0, c1 = c.cta1;
                 __threadfence();
                 __syncwarp();
@@ -764,10 +841,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 // A range that is not finite reaches a row through its score alone, so
                 // that rows that do not see the key stay clear of it.
                 const float vr = scaled_range(to_float<F16>(cur.vr));
-                const uint32_t at = kSlot0 + slot * kSlotBytes + 4 * dt;
+                const uint32_t at = kSlot0 + slot * kSlotBytes + 4 * (((dt >> 1) & 3) * kRangeStride + (dt >> 3) * 2 + (dt & 1));
                 *reinterpret_cast<float*>(smem + at) = cur.real ? to_float<F16>(cur.kr) * p.scale_log2 : 0.0f;
-                *reinterpret_cast<float*>(smem + at + 4 * kN) = cur.real ? __log2f(vr) : -INFINITY;
-                *reinterpret_cast<float*>(smem + at + 8 * kN) = !cur.real ? 0.0f : vr < INFINITY ? __fdividef(1.0f, vr) : 1.0f;
+                *reinterpret_cast<float*>(smem + at + kRangeBytes) = cur.real ? __log2f(vr) : -INFINITY;
+                *reinterpret_cast<float*>(smem + at + 2 * kRangeBytes) = !cur.real ? 0.0f : vr < INFINITY ? __fdividef(1.0f, vr) : 1.0f;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(rfull(slot));
