@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
         *reinterpret_cast<uint4*>(smem + e * 256 + part * 16) = make_uint4(v, v, v, v);
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // after the wait: the tile kernel relies on it
 
     // this CTA's piece [f0, f_end) of the line, and the request it starts in: one
     // scan over the requests, and one more where they are more than the threads

@@ -96,16 +96,15 @@ cudaError_t launch_kv_attention(KvAttendParams p, int head_dim, bool f16, int64_
     uint32_t* counters = reinterpret_cast<uint32_t*>(ws + kWorkspaceBytes);
     const bool tiles = max_q > kTileMinRows / p.group;
     p.tile_rows = tiles ? kTileMinRows : INT64_MAX;
-    if (tiles) {
-        p.counters = counters + kMaxCtas;
-        p.parts = reinterpret_cast<float*>(ws + small_parts_offset() + small_parts_bytes(head_dim));
-        const cudaError_t e = launch_kv_attend_tiles(p, head_dim, f16, s);
-        if (e != cudaSuccess) return e;
-    }
+    const int64_t max_rows = tiles ? kTileMinRows : max_q * p.group;
     p.counters = counters;
     p.parts = reinterpret_cast<float*>(ws + small_parts_offset());
-    const int64_t max_rows = tiles ? kTileMinRows : max_q * p.group;
-    return launch_kv_attend_small(p, head_dim, f16, max_rows, s);
+    const cudaError_t e = launch_kv_attend_small(p, head_dim, f16, max_rows, s);
+    if (e != cudaSuccess || !tiles) return e;
+    // second: it leans on the first's waiting for what came before the call
+    p.counters = counters + kMaxCtas;
+    p.parts = reinterpret_cast<float*>(ws + small_parts_offset() + small_parts_bytes(head_dim));
+    return launch_kv_attend_tiles(p, head_dim, f16, s);
 }
 
 }  // namespace

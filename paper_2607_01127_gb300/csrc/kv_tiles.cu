@@ -62,7 +62,7 @@ constexpr int kThreads = 32 * 16;                // the last warp only completes
 // Registers per thread: 128 at launch; the softmax warps take what the others give back (2 x 160 + 96 + 96 = 4 x 128).
 constexpr int kRegsSoftmax = 160, kRegsDecode = 96, kRegsMma = 96;
 constexpr int kStagesK = 3, kStagesV = 4;        // decoded tiles
-constexpr int kPieceCost = 4;                    // a piece's start and end, in key tiles (~11k cycles)
+constexpr int kPieceCost = 3;                    // a piece's start and end, in key tiles (~7k cycles)
 constexpr int kSlots = 4;                        // tiles' ranges
 constexpr int kMinTiles = 4;                     // key tiles per CTA, at least
 constexpr uint32_t kTabBytes = 256 * 256;        // pair tables: keys in the first, values in the second half of a row
@@ -174,15 +174,14 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
     const uint32_t bar0 = sbase + kBar0;
-    auto kfull = [&](int s) { return bar0 + 8u * s; };                      // decode -> MMA: keys
+    auto kfull = [&](int s) { return bar0 + 8u * s; };                      // decode -> MMA: keys and the tile's ranges
     auto kempty = [&](int s) { return bar0 + 8u * (kStagesK + s); };
     constexpr uint32_t kBv = 2 * kStagesK;
     auto vfull = [&](int s) { return bar0 + 8u * (kBv + s); };              // decode -> MMA: values
     auto vempty = [&](int s) { return bar0 + 8u * (kBv + kStagesV + s); };
     constexpr uint32_t kB1 = kBv + 2 * kStagesV;
-    auto rfull = [&](int s) { return bar0 + 8u * (kB1 + s); };              // decode -> softmax: ranges
-    auto rempty = [&](int s) { return bar0 + 8u * (kB1 + kSlots + s); };
-    constexpr uint32_t kB2 = kB1 + 2 * kSlots;
+    auto rempty = [&](int s) { return bar0 + 8u * (kB1 + s); };          // softmax -> decode: ranges used
+    constexpr uint32_t kB2 = kB1 + kSlots;
     auto sfull = [&](int t) { return bar0 + 8u * (kB2 + t); };              // MMA -> softmax: S
     auto sempty = [&](int t) { return bar0 + 8u * (kB2 + 2 + t); };         // softmax -> MMA: S is in registers
     auto wfull = [&](int t) { return bar0 + 8u * (kB2 + 4 + t); };          // softmax -> MMA: W
@@ -201,9 +200,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     if (tid == 0) {
         for (int s = 0; s < kStagesK; ++s) { mbar_init(kfull(s), kDecWarps); mbar_init(kempty(s), 2); }
         for (int s = 0; s < kStagesV; ++s) { mbar_init(vfull(s), kDecWarps); mbar_init(vempty(s), 2); }
-        for (int s = 0; s < kSlots; ++s) { mbar_init(rfull(s), kDecWarps); mbar_init(rempty(s), kTileWarps); }
+        for (int s = 0; s < kSlots; ++s) mbar_init(rempty(s), kTileWarps);
         for (int t = 0; t < 2; ++t) {
-            mbar_init(sfull(t), 1);
+            mbar_init(sfull(t), 2);
             mbar_init(sempty(t), 4);
             mbar_init(wfull(t), 4);
             mbar_init(wempty(t), 1);
@@ -220,7 +219,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         const uint32_t v = (uint32_t)lv[e & 15] | ((uint32_t)lv[e >> 4] << 16);
         sts128(sbase + e * 256 + part * 16, v, v, v, v);
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // This launch follows the small kernel's of the same call and shares nothing with
+    // it.  It may start when all of that one's CTAs have seen everything before the
+    // call complete (they signal after their own wait), so it does not wait here but
+    // at its end: what comes next waits for this launch, and so for both.
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---------------- this CTA's piece of the line ----------------
@@ -266,7 +268,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     int64_t chunk = (total + gridDim.x - 1) / gridDim.x;
     chunk = chunk < kMinTiles ? kMinTiles : chunk;
     const int64_t f0 = (int64_t)blockIdx.x * chunk, f_end = f0 + chunk < total ? f0 + chunk : total;
-    if (f0 >= f_end) return;                         // the whole CTA
+    if (f0 >= f_end) {                               // the whole CTA
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
     int64_t before = 0;
     for (int64_t base = 0; base < p.requests; base += kThreads) {
         const int64_t w = request_weight(base);
@@ -426,7 +431,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                         for (int k = 0; k < 4; ++k)
                             mma_f16_ss(sa, desc_of(qd + 2 * k), desc_of(kd + (kBlockBytes >> 4) + 2 * k), kIdescS, 1);
                     }
+                    // two arrivals: the products are done, and (an ordinary one, which passes
+                    // on what kfull showed this warp) the key tile's ranges are written
                     mma_commit(sfull(t));
+                    mbar_arrive(sfull(t));
                     mma_commit(kempty(ks));
                 }
                 __syncwarp();
@@ -467,33 +475,38 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         const uint32_t tq = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t ts = tq + kColS + kN * t, tw = tq + kColW + (kN / 2) * t, to = tq + kColO + 128 * t;
         int slot = 0;
-        uint32_t rph = 0, n_s = 0;
+        uint32_t n_s = 0;
         bool ok = true;
+        // The four lanes of a row (16 h + 8 b + g) take neighbouring 16-byte chunks, so
+        // that 64 bytes of it are read at once; chunk 4 i + t's word w goes to column
+        // 16 i + 4 w + t, the order in which the decode warps store dimensions.
         auto load_q = [&](const Piece& c) {
-            const int row = c.row0 + row_in;
-            const bool live = row < c.n * p.group;
-            const uint16_t* src = p.q + (int64_t)(c.q0 + row / p.group) * p.q_stride +
-                                  (int64_t)(c.head * p.group + row % p.group) * D;
-            uint32_t x[32];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (live) v = __ldg(reinterpret_cast<const uint4*>(src) + i);
-                x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
-            }
-            tmem_st_pairs(tq + kColQ + 32 * t, x);
-            if constexpr (D == 128) {
-                // the upper half goes to shared memory: 128-byte rows, swizzled
-                const int m = (warp & 3) * 32 + lane;
-                const uint32_t rb = sbase + kQ0 + t * kQBytes + m * 128;
+            for (int h = 0; h < 2; ++h) {
+                uint32_t x[16];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (live) v = __ldg(reinterpret_cast<const uint4*>(src + 64) + i);
-                    sts128(rb + 16 * (i ^ (m & 7)), v.x, v.y, v.z, v.w);
+                for (int b = 0; b < 2; ++b) {
+                    const int m = (warp & 3) * 32 + 16 * h + 8 * b + (lane >> 2);
+                    const int row = c.row0 + t * 128 + m;
+                    const bool live = row < c.n * p.group;
+                    const uint16_t* src = p.q + (int64_t)(c.q0 + row / p.group) * p.q_stride +
+                                          (int64_t)(c.head * p.group + row % p.group) * D + 8 * (lane & 3);
+                    const uint32_t rb = sbase + kQ0 + t * kQBytes + m * 128 + 4 * (lane & 3);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (live) v = __ldg(reinterpret_cast<const uint4*>(src + 32 * i));
+                        const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            if (i < 2) x[2 * (4 * i + w) + b] = y[w];
+                            else sts32(rb + 16 * ((4 * (i - 2) + w) ^ (m & 7)), y[w]);     // upper half: shared memory, swizzled
+                        }
+                    }
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tmem_st_pairs_frag(tq + kColQ + 32 * t + ((uint32_t)(16 * h) << 16), x);
             }
+            if constexpr (D == 128) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
@@ -523,11 +536,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             for (int i = 0; i < 4; ++i) { ref[i] = kRefInit; sum[i] = make_float2(0.0f, 0.0f); }
             for (int j = c.j0; j < c.j1; ++j) {
                 const int kb = (c.lo_tile + j) * kN;
-                if (!warp_poll(rfull(slot), rph, p.ws, kWaitSoftmax) ||
-                    !warp_poll(sfull(t), n_s & 1u, p.ws, kWaitSoftmax)) {
-                    ok = false;
-                    break;
-                }
+                ok = warp_poll(sfull(t), n_s & 1u, p.ws, kWaitSoftmax);
+                if (!ok) break;
                 ++n_s;
                 tc_fence_after();
                 const uint32_t rg = sbase + kSlot0 + slot * kSlotBytes + (lane & 3) * (kRangeStride * 4);
@@ -637,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                     mbar_arrive(wfull(t));
                     mbar_arrive(rempty(slot));
                 }
-                if (++slot == kSlots) { slot = 0; rph ^= 1u; }
+                if (++slot == kSlots) slot = 0;
             }
             if (!ok) break;
             // the piece's last S is read, so Q may be replaced and the next piece begin
@@ -645,50 +655,58 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             if (more) load_q(c_next);
             if (!warp_poll(wempty(t), (n_s & 1u) ^ 1u, p.ws, kWaitSoftmax)) break;
             tc_fence_after();
-            // from here a lane has the row of its number: fetch that row's sum and reference
-            const int row = c.row0 + row_in;
-            float row_ref = 0.0f, row_sum = 0.0f;
+            const bool whole = c.whole != 0;
+            float* part = p.parts + (size_t)(2 * blockIdx.x + c.starts) * tile_slot_floats(D);
+            float row_sum[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float l = sum[i].x + sum[i].y;
                 l += __shfl_xor_sync(0xffffffffu, l, 1);
-                l += __shfl_xor_sync(0xffffffffu, l, 2);
-                const float a = __shfl_sync(0xffffffffu, l, 4 * (lane & 7)), b = __shfl_sync(0xffffffffu, ref[i], 4 * (lane & 7));
-                if (lane >> 3 == i) row_sum = a, row_ref = b;
+                row_sum[i] = l + __shfl_xor_sync(0xffffffffu, l, 2);
             }
-            const bool whole = c.whole != 0;
-            const bool live = row < c.n * p.group;
-            float* part = p.parts + (size_t)(2 * blockIdx.x + c.starts) * tile_slot_floats(D);
-            uint16_t* dst = p.out + ((int64_t)(c.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group +
-                                     row % p.group) * D;
-            const float inv = row_sum == 0.0f ? 0.0f : 1.0f / row_sum;
+            // a lane's fragments of a row are 16 contiguous bytes of 16-bit results per 32 dimensions
 #pragma unroll 1
-            for (int h = 0; h < D / 32; ++h) {
-                uint32_t o[32];
-                tmem_ld32(to + 32 * h, o);
-                if (whole) {
-                    if (live) {
+            for (int h = 0; h < D / 32; ++h) {           // 64 columns of the lower, then of the upper 16 rows
+                float o[32];
+                tmem_ld_frag(to + 64 * (h >> 1) + ((uint32_t)((h & 1) * 16) << 16), o);
+                tmem_wait_frag(o);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t y[4];
+                for (int b = 0; b < 2; ++b) {
+                    const int m = t * 128 + (warp & 3) * 32 + 16 * (h & 1) + 8 * b + (lane >> 2);
+                    const int row = c.row0 + m;
+                    const float l = h & 1 ? row_sum[2 + b] : row_sum[b];
+                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                    uint16_t* dst = p.out + ((int64_t)(c.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group +
+                                             row % p.group) * D + 64 * (h >> 1) + 8 * (lane & 3);
+                    float* keep = part + (size_t)m * D + 64 * (h >> 1) + 8 * (lane & 3);
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                y[k] = pack2<F16>(__uint_as_float(o[8 * i + 2 * k]) * inv, __uint_as_float(o[8 * i + 2 * k + 1]) * inv);
-                            *(reinterpret_cast<uint4*>(dst + 32 * h) + i) = make_uint4(y[0], y[1], y[2], y[3]);
+                    for (int i = 0; i < 2; ++i) {
+                        float y[8];
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            y[2 * w] = o[4 * (4 * i + w) + 2 * b];
+                            y[2 * w + 1] = o[4 * (4 * i + w) + 2 * b + 1];
+                        }
+                        if (!whole) {
+                            __stcg(reinterpret_cast<float4*>(keep + 32 * i), make_float4(y[0], y[1], y[2], y[3]));
+                            __stcg(reinterpret_cast<float4*>(keep + 32 * i) + 1, make_float4(y[4], y[5], y[6], y[7]));
+                        } else if (row < c.n * p.group) {
+                            *reinterpret_cast<uint4*>(dst + 32 * i) =
+                                make_uint4(pack2<F16>(y[0] * inv, y[1] * inv), pack2<F16>(y[2] * inv, y[3] * inv),
+                                           pack2<F16>(y[4] * inv, y[5] * inv), pack2<F16>(y[6] * inv, y[7] * inv));
                         }
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        __stcg(reinterpret_cast<uint4*>(part + (size_t)row_in * D + 32 * h) + i,
-                               make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]));
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(oempty(t));
             if (!whole) {
-                __stcg(reinterpret_cast<float2*>(part + (size_t)kTileRows * D) + row_in, make_float2(row_ref, row_sum));
+                if ((lane & 3) == 0)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        __stcg(reinterpret_cast<float2*>(part + (size_t)kTileRows * D) + t * 128 + (warp & 3) * 32 + 8 * i + (lane >> 2),
+                               make_float2(ref[i], row_sum[i]));
                 const int c0 = c.cta0, c1 = c.cta1;
                 __threadfence();
                 __syncwarp();
@@ -707,7 +725,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                     const float li = l == 0.0f ? 0.0f : 1.0f / l;
                     // a row's dimensions across the lanes, so that the parts are read in whole lines
                     constexpr int kLanes = D / 4, kPer = 32 / kLanes;
-                    const int64_t off = live ? (int64_t)(dst - p.out) : -1;
+                    const int row = c.row0 + row_in;
+                    const int64_t off = row >= c.n * p.group ? -1 :
+                        ((int64_t)(c.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group + row % p.group) * D;
                     const int d = (lane % kLanes) * 4;
 #pragma unroll 1
                     for (int i0 = 0; i0 < 32; i0 += 8 * kPer) {
@@ -819,9 +839,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
 #pragma unroll
                 for (int q = 0; q < 16; ++q) y[q] = lds_tab(prmt(x[q / 4], which, 0x7604u + 0x10u * (q % 4)));
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < 4; ++q) {        // word 4 q + i of the 16 holds dimensions 2 (4 i + q), + 1
                     const uint32_t c16 = (uint32_t)((chunk_i & 1) * 4 + q) ^ (uint32_t)(row & 7);
-                    sts128(rb + c16 * 16, y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]);
+                    sts128(rb + c16 * 16, y[q], y[4 + q], y[8 + q], y[12 + q]);
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // visible to the MMA's reads
@@ -846,8 +866,6 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 *reinterpret_cast<float*>(smem + at + kRangeBytes) = cur.real ? __log2f(vr) : -INFINITY;
                 *reinterpret_cast<float*>(smem + at + 2 * kRangeBytes) = !cur.real ? 0.0f : vr < INFINITY ? __fdividef(1.0f, vr) : 1.0f;
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(rfull(slot));
             if (++slot == kSlots) { slot = 0; rph ^= 1u; }
             ok = warp_poll(kempty(ks), kph ^ 1u, p.ws, kWaitDecode);
             if (!ok) break;
@@ -873,6 +891,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 template <int D, bool F16>
