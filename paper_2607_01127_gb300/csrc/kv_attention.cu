@@ -48,6 +48,7 @@ namespace {
 constexpr int kStep = 16;                    // keys per warp step
 constexpr int kMinChunk = 20;                // places of the line per CTA, at least
 constexpr int kPieceCost = 12;               // joining a piece's warps, in steps (~1.3 us)
+constexpr int kWholeSteps = 64;              // a segment of so few steps stays whole: joining its parts takes 3.4 us
 constexpr uint32_t kTabBytes = 256 * 256;
 
 // Launch shapes by columns (8 NT): a batch-1 group of up to 8 query heads leaves
@@ -255,9 +256,11 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
 
     for (; line < f_end; ) {
         const int64_t at = line + kPieceCost, seg_end = at + rq.steps;
-        const int sb = f0 > at ? (int)(f0 - at) : 0;
-        const int se = f_end < seg_end ? (int)(f_end - at) : rq.steps;
-        if (sb < se) {
+        const int cta = (int)blockIdx.x, places = rq.steps + kPieceCost;
+        const Sharing sh = share_segment(line, places, rq.steps <= kWholeSteps ? places / 2 : kPieceCost + 8, chunk);
+        if (cta >= sh.first && cta <= sh.last) {
+        const int sb = cta == sh.first ? 0 : (int)(f0 - at);
+        const int se = cta == sh.last ? rq.steps : (int)(f0 + chunk - at);
         const int row0 = block * NC;                     // first query row (token * group + head in group)
         const int rows = rq.n * p.group - row0 < NC ? rq.n * p.group - row0 : NC;
         const int kv = (int)rq.kv, hi = (int)rq.hi, window = (int)p.window;
@@ -457,9 +460,9 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
                 for (int x = 4; x < 32; x <<= 1) v += __shfl_xor_sync(0xffffffffu, v, x);
                 if (g == 0) stat[warp * NC + nt * 8 + 2 * t + c] = make_float2(ref[nt][c], v);
             }
-        const bool whole = sb == 0 && se == rq.steps;
+        const bool whole = sh.first == sh.last;
         // this piece's slot: the second of the CTA's two when the segment starts here
-        float* part = p.parts + (size_t)(2 * blockIdx.x + (sb == 0 ? 1 : 0)) * slot_floats(D);
+        float* part = p.parts + (size_t)(2 * cta + (cta == sh.first ? 1 : 0)) * slot_floats(D);
         auto write_out = [&](int col, int d, const float4& v, float l) {
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
             const int row = row0 + col;
@@ -503,7 +506,7 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
         }
         if (!whole) {
             // the last CTA of the segment to arrive joins the parts in key order
-            const int c0 = (int)(at / chunk), n = (int)((seg_end - 1) / chunk) - c0 + 1;
+            const int c0 = sh.first, n = sh.last - sh.first + 1;
             __threadfence();
             __syncthreads();
             if (tid == 0)
@@ -514,19 +517,27 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
                 auto part_of = [&](int x) { return p.parts + (size_t)(2 * (c0 + x) + (x == 0 ? 1 : 0)) * slot_floats(D); };
                 for (int i = tid; i < n * NC; i += kThreads)
                     if (i % NC < rows) pstat[i] = __ldcg(reinterpret_cast<const float2*>(part_of(i / NC) + kMaxCols * D) + i % NC);
-                __syncthreads();
-                for (int i = tid; i < rows * (D / 4); i += kThreads) {
-                    const int col = i / (D / 4), d = (i % (D / 4)) * 4;
+                // every thread joins four dimensions of a column; the first eight parts
+                // are on their way while the statistics arrive
+                for (int i0 = 0; i0 < rows * (D / 4); i0 += kThreads) {
+                    const int i = i0 + tid;
+                    const bool mine = i < rows * (D / 4);
+                    const int col = mine ? i / (D / 4) : 0, d = (i % (D / 4)) * 4;
+                    float4 y[8];
+                    auto fetch = [&](int x0) {
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            y[x] = mine && x0 + x < n ? __ldcg(reinterpret_cast<const float4*>(part_of(x0 + x) + col * D + d))
+                                                      : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    };
+                    fetch(0);
+                    if (i0 == 0) __syncthreads();
                     float m = kRefInit;
                     for (int x = 0; x < n; ++x) m = fmaxf(m, pstat[x * NC + col].x);
                     float l = 0.0f;
                     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                     for (int x0 = 0; x0 < n; x0 += 8) {
-                        float4 y[8];
-#pragma unroll
-                        for (int x = 0; x < 8; ++x)
-                            y[x] = x0 + x < n ? __ldcg(reinterpret_cast<const float4*>(part_of(x0 + x) + col * D + d))
-                                              : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (x0) fetch(x0);
 #pragma unroll
                         for (int x = 0; x < 8; ++x) {
                             if (x0 + x >= n) break;
@@ -536,7 +547,7 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
                             v.x += y[x].x * k; v.y += y[x].y * k; v.z += y[x].z * k; v.w += y[x].w * k;
                         }
                     }
-                    write_out(col, d, v, l);
+                    if (mine) write_out(col, d, v, l);
                 }
             }
             __syncthreads();

@@ -45,6 +45,21 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
 // kept above 2^-100, below which their reciprocals leave fp32.  NaN stays.
 __device__ __forceinline__ float scaled_range(float r) { return r == 0.0f ? 0x1p-60f : r < 0x1p-100f ? 0x1p-100f : r; }
 
+// How a segment [line, line + places) is shared by CTAs whose raw pieces are
+// `chunk` places each.  A cut next to either end moves there, and every cut of a
+// short segment does, because parts cost a join (they go through global memory).
+struct Sharing {
+    int first, last;         // CTAs: the segment is one CTA's where they are equal
+};
+__device__ __forceinline__ Sharing share_segment(int64_t line, int places, int margin, int64_t chunk)
+{
+    Sharing s;
+    s.first = (int)((line + margin) / chunk);
+    const int last = (int)((line + places - margin + chunk - 1) / chunk) - 1;
+    s.last = last > s.first ? last : s.first;
+    return s;
+}
+
 // A request as the attention kernels see it, its lengths made safe to index with.
 struct Request {
     int32_t q0, n;           // first token, tokens

@@ -62,6 +62,7 @@ constexpr int kThreads = 32 * 16;                // the last warp only completes
 // Registers per thread: 128 at launch; the softmax warps take what the others give back (2 x 160 + 96 + 96 = 4 x 128).
 constexpr int kRegsSoftmax = 160, kRegsDecode = 96, kRegsMma = 96;
 constexpr int kStagesK = 3, kStagesV = 4;        // decoded tiles
+constexpr int kWholeTiles = 12;                  // a segment of so few key tiles stays whole: its parts would be joined
 constexpr int kPieceCost = 3;                    // a piece's start and end, in key tiles (~7k cycles)
 constexpr int kSlots = 4;                        // tiles' ranges
 constexpr int kMinTiles = 4;                     // key tiles per CTA, at least
@@ -377,22 +378,26 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             bool ok = true;
             while (ok && line < f_end) {
                 const int64_t at = line + kPieceCost, end = at + tiles;
-                Piece c{};
-                c.r = (int)r;
-                c.q0 = rq.q0;
-                c.n = rq.n;
-                c.kv = (int)rq.kv;
-                c.hi = (int)rq.hi;
-                c.row0 = block * kTileRows;
-                c.head = head;
-                c.lo_tile = lo_tile;
-                c.j0 = f0 > at ? (int)(f0 - at) : 0;
-                c.j1 = f_end < end ? (int)(f_end - at) : tiles;
-                c.whole = c.j0 == 0 && c.j1 == tiles;
-                c.cta0 = (int)(at / chunk);
-                c.cta1 = (int)((end - 1) / chunk);
-                c.starts = c.j0 == 0;
-                if (c.j0 < c.j1) ok = announce(c);
+                const int cta = (int)blockIdx.x, places = tiles + kPieceCost;
+                const Sharing sh = share_segment(line, places, tiles <= kWholeTiles ? places / 2 : kPieceCost + 2, chunk);
+                if (cta >= sh.first && cta <= sh.last) {
+                    Piece c{};
+                    c.r = (int)r;
+                    c.q0 = rq.q0;
+                    c.n = rq.n;
+                    c.kv = (int)rq.kv;
+                    c.hi = (int)rq.hi;
+                    c.row0 = block * kTileRows;
+                    c.head = head;
+                    c.lo_tile = lo_tile;
+                    c.j0 = cta == sh.first ? 0 : (int)(f0 - at);
+                    c.j1 = cta == sh.last ? tiles : (int)(f0 + chunk - at);
+                    c.whole = sh.first == sh.last;
+                    c.cta0 = sh.first;
+                    c.cta1 = sh.last;
+                    c.starts = cta == sh.first;
+                    ok = announce(c);
+                }
                 line = end;
                 if (line < f_end && ++head == p.heads) {
                     head = 0;
