@@ -66,11 +66,12 @@ __host__ __device__ constexpr size_t merge_bytes()
     return o > parts ? o : parts;
 }
 
+// The tables do not change once they are built, so the look-ups may be scheduled freely.
 template <uint32_t OFF>
 __device__ __forceinline__ uint32_t lds_tab(uint32_t off)
 {
     uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1+%2];" : "=r"(v) : "r"(off), "n"(kTabOff + OFF));
+    asm("ld.shared.u32 %0, [%1+%2];" : "=r"(v) : "r"(off), "n"(kTabOff + OFF));
     return v;
 }
 
@@ -79,11 +80,11 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
                                          uint32_t b1)
 {
     if constexpr (F16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -339,11 +340,11 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
         auto compute = [&](const StepData<D>& cur, int s) {
             const int kb = (rq.lo_step + s) * kStep;
             // S^T = K Q^T
-            float acc[NT][4];
+            float acc[NT][4], acc2[NT][4];               // two chains of products
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[nt][c] = 0.0f;
+                for (int c = 0; c < 4; ++c) acc[nt][c] = acc2[nt][c] = 0.0f;
 #pragma unroll
             for (int w = 0; w < D / 32; ++w) {
                 uint32_t a[2][4];
@@ -357,7 +358,7 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     mma16816<F16>(acc[nt], a[0][0], a[1][0], a[0][1], a[1][1], qf[nt][4 * w], qf[nt][4 * w + 1]);
-                    mma16816<F16>(acc[nt], a[0][2], a[1][2], a[0][3], a[1][3], qf[nt][4 * w + 2], qf[nt][4 * w + 3]);
+                    mma16816<F16>(acc2[nt], a[0][2], a[1][2], a[0][3], a[1][3], qf[nt][4 * w + 2], qf[nt][4 * w + 3]);
                 }
             }
 
@@ -367,16 +368,19 @@ __global__ void __launch_bounds__(32 * warps_of<NT>, ctas_per_sm<NT>) attend_ker
             for (int h = 0; h < 2; ++h) {
                 ks[h] = to_float<F16>(cur.kr[h]) * p.scale_log2;
                 const float vr = scaled_range(to_float<F16>(cur.vr[h]));
-                lv[h] = __log2f(vr);
-                iv[h] = vr < INFINITY ? __fdividef(1.0f, vr) : 1.0f;
+                lv[h] = log2_approx(vr);
+                iv[h] = rcp_approx(vr);
             }
             const bool masked = cur.bad || kb + kStep - 1 > all_hi || kb < all_lo;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[nt][c] = fmaf(acc[nt][c], ks[c >> 1], lv[c >> 1]);
+                for (int c = 0; c < 4; ++c) acc[nt][c] = fmaf(acc[nt][c] + acc2[nt][c], ks[c >> 1], lv[c >> 1]);
             if (masked) {
-                // a hidden key's range may be anything, NaN included: its score is replaced
+                // a hidden key's range may be anything, NaN included: its score is replaced,
+                // and what multiplies its weight of zero is finite
+                iv[0] = iv[0] < INFINITY ? iv[0] : 1.0f;
+                iv[1] = iv[1] < INFINITY ? iv[1] : 1.0f;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

@@ -40,10 +40,29 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     }
 }
 
+// log2 and 1 / x of a scaled range (normal, or NaN or Inf): abs. error 2^-22, rel. 2^-23
+__device__ __forceinline__ float log2_approx(float x)
+{
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // The range that the weights are scaled by.  A range of zero stands for zeros: any
 // small one gives the same products, and 2^-60 keeps the sums exact; others are
 // kept above 2^-100, below which their reciprocals leave fp32.  NaN stays.
-__device__ __forceinline__ float scaled_range(float r) { return r == 0.0f ? 0x1p-60f : r < 0x1p-100f ? 0x1p-100f : r; }
+__device__ __forceinline__ float scaled_range(float r)
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(r), "f"(0x1p-100f));
+    return r == 0.0f ? 0x1p-60f : m;
+}
 
 // How a segment [line, line + places) is shared by CTAs whose raw pieces are
 // `chunk` places each.  A cut next to either end moves there, and every cut of a

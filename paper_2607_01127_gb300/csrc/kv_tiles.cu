@@ -868,8 +868,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 const float vr = scaled_range(to_float<F16>(cur.vr));
                 const uint32_t at = kSlot0 + slot * kSlotBytes + 4 * (((dt >> 1) & 3) * kRangeStride + (dt >> 3) * 2 + (dt & 1));
                 *reinterpret_cast<float*>(smem + at) = cur.real ? to_float<F16>(cur.kr) * p.scale_log2 : 0.0f;
-                *reinterpret_cast<float*>(smem + at + kRangeBytes) = cur.real ? __log2f(vr) : -INFINITY;
-                *reinterpret_cast<float*>(smem + at + 2 * kRangeBytes) = !cur.real ? 0.0f : vr < INFINITY ? __fdividef(1.0f, vr) : 1.0f;
+                *reinterpret_cast<float*>(smem + at + kRangeBytes) = cur.real ? log2_approx(vr) : -INFINITY;
+                *reinterpret_cast<float*>(smem + at + 2 * kRangeBytes) = !cur.real ? 0.0f : vr < INFINITY ? rcp_approx(vr) : 1.0f;
             }
             if (++slot == kSlots) { slot = 0; rph ^= 1u; }
             ok = warp_poll(kempty(ks), kph ^ 1u, p.ws, kWaitDecode);
