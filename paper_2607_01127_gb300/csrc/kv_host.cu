@@ -69,10 +69,14 @@ logq_status status_of(cudaError_t e)
     return e == cudaSuccess ? LOGQ_OK : LOGQ_ERR_CUDA;
 }
 
-// Requests with at most this many query rows (tokens x query heads per kv head)
-// run on the small kernel, which re-reads the keys for every 16 of them; the
-// tiles of the large one hold 256.
-constexpr int64_t kTileMinRows = 64;
+// Requests with at most kTileMinRows query rows (tokens x query heads per kv head)
+// run on the small kernel, which re-reads the keys for every 24 of them; the tiles
+// of the large one hold 256.  Measured with 8 kv heads x 128: 16 requests of 48 rows
+// and 2000 keys 39 us on the small and 66 us on the large kernel, of 96 rows 67 and
+// 66, of 160 rows 108 and 66; 64 requests of 48 rows and 500 keys 53 and 74, of 96
+// rows 103 and 74.  A call of at most kTileMinTotal rows in all does not fill the
+// large kernel's tiles: one request of 96 rows and 4000 keys takes 19 and 55 us.
+constexpr int64_t kTileMinRows = 64, kTileMinTotal = 128;
 
 int sms_or_default() { return sm_count() > 0 ? sm_count() : 148; }
 
@@ -94,7 +98,7 @@ cudaError_t launch_kv_attention(KvAttendParams p, int head_dim, bool f16, int64_
 {
     uint8_t* ws = reinterpret_cast<uint8_t*>(p.ws);
     uint32_t* counters = reinterpret_cast<uint32_t*>(ws + kWorkspaceBytes);
-    const bool tiles = max_q > kTileMinRows / p.group;
+    const bool tiles = max_q > kTileMinRows / p.group && p.tokens * p.group > kTileMinTotal;
     p.tile_rows = tiles ? kTileMinRows : INT64_MAX;
     const int64_t max_rows = tiles ? kTileMinRows : max_q * p.group;
     p.counters = counters;

@@ -692,10 +692,11 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                             y[2 * w] = o[4 * (4 * i + w) + 2 * b];
                             y[2 * w + 1] = o[4 * (4 * i + w) + 2 * b + 1];
                         }
+                        if (row >= c.n * p.group) continue;
                         if (!whole) {
                             __stcg(reinterpret_cast<float4*>(keep + 32 * i), make_float4(y[0], y[1], y[2], y[3]));
                             __stcg(reinterpret_cast<float4*>(keep + 32 * i) + 1, make_float4(y[4], y[5], y[6], y[7]));
-                        } else if (row < c.n * p.group) {
+                        } else {
                             *reinterpret_cast<uint4*>(dst + 32 * i) =
                                 make_uint4(pack2<F16>(y[0] * inv, y[1] * inv), pack2<F16>(y[2] * inv, y[3] * inv),
                                            pack2<F16>(y[4] * inv, y[5] * inv), pack2<F16>(y[6] * inv, y[7] * inv));
@@ -706,7 +707,8 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(oempty(t));
-            if (!whole) {
+            // (a warp whose rows do not exist has written nothing that matters and joins nothing)
+            if (!whole && c.row0 + t * 128 + (warp & 3) * 32 < c.n * p.group) {
                 if ((lane & 3) == 0)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -739,16 +741,26 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                         float4 y[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) y[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        for (int x = c0; x <= c1; ++x) {
-                            const float k = exp2_approx(stat_of(x).x - m) * li;
-                            const float* src = part_of(x) + (size_t)(row_in - lane + i0 + lane / kLanes) * D + d;
-                            float4 a[8];
+                        for (int x0 = c0; x0 <= c1; x0 += 2) {       // two parts' loads on their way at a time
+                            float k[2];
+                            float4 a[2][8];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) a[i] = __ldcg(reinterpret_cast<const float4*>(src + i * kPer * D));
+                            for (int z = 0; z < 2; ++z) {
+                                const int x = x0 + z <= c1 ? x0 + z : c1;
+                                const float* src = part_of(x) + (size_t)(row_in - lane + i0 + lane / kLanes) * D + d;
+                                k[z] = stat_of(x).x;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const float f = __shfl_sync(0xffffffffu, k, i0 + i * kPer + lane / kLanes);
-                                y[i].x += a[i].x * f; y[i].y += a[i].y * f; y[i].z += a[i].z * f; y[i].w += a[i].w * f;
+                                for (int i = 0; i < 8; ++i) a[z][i] = __ldcg(reinterpret_cast<const float4*>(src + i * kPer * D));
+                            }
+#pragma unroll
+                            for (int z = 0; z < 2; ++z) {
+                                if (x0 + z > c1) break;
+                                const float kz = exp2_approx(k[z] - m) * li;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    const float f = __shfl_sync(0xffffffffu, kz, i0 + i * kPer + lane / kLanes);
+                                    y[i].x += a[z][i].x * f; y[i].y += a[z][i].y * f; y[i].z += a[z][i].z * f; y[i].w += a[z][i].w * f;
+                                }
                             }
                         }
 #pragma unroll
