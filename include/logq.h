@@ -468,7 +468,11 @@ size_t logq_kv_attention_workspace_bytes(int32_t q_heads, int32_t kv_heads, int3
  *   max_q: an upper bound of a request's tokens in this call; it only chooses
  *   kernels (any value gives the same results up to rounding).
  * Scores, softmax and sums are fp32; the weights that multiply the values are
- * rounded to fp16 (scaled by the value's range, so that none overflows).
+ * rounded to fp16 (scaled by the value's range, so that none overflows; nonzero
+ * ranges below 2^-100 count as 2^-100).  Key ranges of a request may be shared by
+ * several CTAs, whose parts are joined in a fixed order: results do not depend on
+ * timing.  A device-side wait that hit its bound is reported later by
+ * logq_workspace_status(workspace); zero the workspace before using it again.
  * Asynchronous.  Errors: LOGQ_ERR_INVALID_ARG, LOGQ_ERR_UNSUPPORTED,
  * LOGQ_ERR_WORKSPACE, LOGQ_ERR_CUDA. */
 logq_status logq_kv_attention(const logq_kv_cache* cache, const void* q, int64_t q_stride, int32_t q_heads,

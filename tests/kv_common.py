@@ -89,7 +89,7 @@ def attention_ref(cache, q, q_start, kv_len, table, scale, window, k_base, v_bas
     out = torch.full((tokens, hq, d), float("nan"), dtype=torch.float64, device=dev)
     bound = torch.zeros_like(out)
     half = 2.0 ** -8 if q.dtype == torch.bfloat16 else 2.0 ** -11
-    starts, kvs = [min(max(int(x), 0), tokens) for x in q_start], [int(x) for x in kv_len]
+    starts, kvs = [int(x) for x in q_start], [int(x) for x in kv_len]
     for r in range(len(kvs)):
         a, b = starts[r], starts[r + 1]
         n, kv = b - a, max(kvs[r], 0)

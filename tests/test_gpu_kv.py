@@ -329,3 +329,58 @@ def test_step_on_another_stream_and_in_a_graph():
         graph.replay()
         check(*got)
     assert got[1].tolist() == [38, 5, 36]
+
+
+def test_example_layer():
+    """The example's layer: every step's attention against 64 bits over what its cache holds."""
+    import os
+    import sys
+    lib()
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import paged_decode
+
+    seen = []
+
+    def check(layer, q, out, q_start, kv_len, table):
+        check_attention(out, *attention_ref(layer.cache, q, q_start.tolist(), kv_len.tolist(), table,
+                                            layer.DIM ** -0.5, 0, 1.5, 1.5))
+        seen.append(kv_len.tolist())
+
+    y, ctx, layer = paged_decode.run(steps=6, check=check)
+    assert y.isfinite().all() and seen[0] == [40, 3, 117, 64]
+    assert ctx.tolist() == [25 + 2, 3 + 6, 117 + 6, 64 + 6]
+    held = sum(up(n, 16) for n in ctx.tolist())
+    assert int(layer.ring_state[1]) == layer.cache.pages - held
+    # every page is either held once or free once
+    free = layer.ring[(int(layer.ring_state[0]) + torch.arange(int(layer.ring_state[1]), device="cuda")) % layer.ring.numel()]
+    used = torch.cat([t[:up(n, 16)] for t, n in zip(layer.block_table, ctx.tolist())])
+    assert torch.equal(torch.cat([free, used]).sort().values, torch.arange(layer.cache.pages, dtype=torch.int32, device="cuda"))
+
+
+
+def test_empty_calls():
+    logq = lib()
+    cache = logq.new_kv_cache(4, 16, 2, 64, BF)
+    none = torch.empty(0, 2, 64, dtype=BF, device="cuda")
+    assert logq.logq_kv_append(cache, none, none, torch.empty(0, dtype=torch.int64, device="cuda")) is None
+    q = torch.empty(0, 4, 64, dtype=BF, device="cuda")
+    assert logq.logq_kv_attention(cache, q, i32([0, 0]), i32([7]), i32([[0]])).shape == (0, 4, 64)
+    q = torch.ones(3, 4, 64, dtype=BF, device="cuda")
+    out = torch.full_like(q, 5.0)
+    logq.logq_kv_attention(cache, q, i32([0]), i32([]), torch.empty(0, 1, dtype=torch.int32, device="cuda"), out=out)
+    assert (out == 5).all()
+
+
+@pytest.mark.parametrize("tokens", [10, 300])
+def test_attention_odd_bounds(tokens):
+    """Bounds that do not ascend or leave the tokens are cut to them; a negative length is none."""
+    logq = lib()
+    cache, gen = filled(logq, 16, 32, 2, 64, FH, 6)
+    table = torch.arange(16, dtype=torch.int32, device="cuda").view(4, 4)
+    q = torch.randn(tokens, 4, 64, generator=gen, device="cuda").to(FH)
+    q_start, kv = [tokens // 2, 2, -7, tokens - 1, 10 ** 6], [100, -5, 128, 90]
+    # requests: none (from the middle back to 2), none, tokens 0 .. n - 2, the last token
+    out = torch.full_like(q, 5.0)
+    logq.logq_kv_attention(cache, q, i32(q_start), i32(kv), table, out=out)
+    check_attention(out, *attention_ref(cache, q, [tokens, tokens, 0, tokens - 1, tokens], [100, 0, 128, 90], table,
+                                        64 ** -0.5, 0, KB, VB))
