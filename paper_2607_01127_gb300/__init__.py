@@ -22,6 +22,7 @@ load it).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -423,6 +424,18 @@ def _raw_stream(stream, index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index)
 
 
+_NOWHERE = contextlib.nullcontext()
+
+
+def _made_on(stream):
+    """Where a call's own tensors are made: on the stream it runs on, so that their zero-fill is
+    ordered before it and their memory is not handed out again while it runs."""
+    if stream is None:
+        return _NOWHERE
+    import torch
+    return torch.cuda.stream(stream)
+
+
 def _check_int32(index: int, *tensors) -> None:
     import torch
     for x in tensors:
@@ -493,14 +506,12 @@ def logq_kv_plan(ctx_len, new_len, block_table, ring, ring_state, page_size: int
     _check_int32(index, ctx_len, new_len, block_table, ring, ring_state)
     assert new_len.numel() == n and block_table.dim() == 2 and block_table.shape[0] == n and ring_state.numel() == 2
     dev, i32, empty = ctx_len.device, torch.int32, torch.empty     # (a view costs more than an allocation)
-    q_start, kv_len = empty(n + 1, dtype=i32, device=dev), empty(n, dtype=i32, device=dev)
-    positions, slots = empty(max_tokens, dtype=i32, device=dev), empty(max_tokens, dtype=torch.int64, device=dev)
-    if inplace:
-        out = ring_state
-        if workspace is None:
+    with _made_on(stream):
+        q_start, kv_len = empty(n + 1, dtype=i32, device=dev), empty(n, dtype=i32, device=dev)
+        positions, slots = empty(max_tokens, dtype=i32, device=dev), empty(max_tokens, dtype=torch.int64, device=dev)
+        out = ring_state if inplace else empty(2, dtype=i32, device=dev)
+        if inplace and workspace is None:
             workspace = new_workspace(dev)
-    else:
-        out = empty(2, dtype=i32, device=dev)
     st = _lib().logq_kv_plan(ctx_len.data_ptr(), new_len.data_ptr(), n, block_table.data_ptr(), block_table.shape[1],
                              page_size, ring.data_ptr(), ring.numel(), ring_state.data_ptr(), out.data_ptr(),
                              max_tokens, q_start.data_ptr(), kv_len.data_ptr(), positions.data_ptr(),
@@ -530,8 +541,9 @@ def logq_kv_append(cache: KVCache, k, v, slots, values: bool = False, stream=Non
         and slots.get_device() == index, "slots: a contiguous int64 device tensor, one per token"
     kv = vv = None
     if values:
-        kv = torch.empty((n, heads, dim), dtype=cache.dtype, device=cache.device)
-        vv = torch.empty((n, heads, dim), dtype=cache.dtype, device=cache.device)
+        with _made_on(stream):
+            kv = torch.empty((n, heads, dim), dtype=cache.dtype, device=cache.device)
+            vv = torch.empty((n, heads, dim), dtype=cache.dtype, device=cache.device)
     st = _lib().logq_kv_append(cache._ref, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), n,
                                kv.data_ptr() if values else None, vv.data_ptr() if values else None,
                                _raw_stream(stream, index))
@@ -550,12 +562,13 @@ def logq_kv_attention(cache: KVCache, q, q_start, kv_len, block_table, scale: fl
     qs = _rows(q, hq, dim, cache, "q")
     _check_int32(index, q_start, kv_len, block_table)
     assert q_start.numel() == n + 1 and block_table.dim() == 2 and block_table.shape[0] == n
-    if out is None:
-        out = torch.empty((tokens, hq, dim), dtype=cache.dtype, device=cache.device)
-    else:
-        assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
-    if workspace is None:
-        workspace = new_kv_workspace(hq, cache.heads, dim, cache.device)
+    with _made_on(stream):
+        if out is None:
+            out = torch.empty((tokens, hq, dim), dtype=cache.dtype, device=cache.device)
+        else:
+            assert out.shape == q.shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == index
+        if workspace is None:
+            workspace = new_kv_workspace(hq, cache.heads, dim, cache.device)
     st = _lib().logq_kv_attention(cache._ref, q.data_ptr(), qs, hq, tokens, q_start.data_ptr(), kv_len.data_ptr(), n,
                                   block_table.data_ptr(), block_table.shape[1], dim ** -0.5 if scale is None else scale,
                                   window, tokens if max_q is None else max_q, out.data_ptr(), workspace.data_ptr(),

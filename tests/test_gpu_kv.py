@@ -384,3 +384,37 @@ def test_attention_odd_bounds(tokens):
     logq.logq_kv_attention(cache, q, i32(q_start), i32(kv), table, out=out)
     check_attention(out, *attention_ref(cache, q, [tokens, tokens, 0, tokens - 1, tokens], [100, 0, 128, 90], table,
                                         64 ** -0.5, 0, KB, VB))
+
+
+@pytest.mark.parametrize("heavy", [150, 9, 1])
+def test_attention_of_many_requests(heavy):
+    """More requests than a CTA has threads: the scans over them go round."""
+    logq = lib()
+    q_lens, kv_lens = [1] * 700, [1 + (7 * i) % 40 for i in range(700)]
+    for i in (0, 300, 699):
+        q_lens[i], kv_lens[i] = heavy, heavy + 90
+    q_lens[5] = 0
+    cache, gen = filled(logq, sum(up(m, 16) for m in kv_lens), 16, 2, 64, BF, 8)
+    check_attention(*attend(logq, cache, gen, q_lens, kv_lens, 8))
+
+
+def test_stream_argument_orders_a_calls_own_tensors():
+    """With stream=, what a call makes for itself is made there: its workspace's zero-fill comes before
+    the kernels, and its memory is not given to the current stream while they run."""
+    logq = lib()
+    cache, gen = filled(logq, 64, 64, 8, 128, BF, 12)
+    side = torch.cuda.Stream()
+    q = torch.randn(300, 32, 128, generator=gen, device="cuda").to(BF)
+    table = torch.arange(64, dtype=torch.int32, device="cuda").view(1, 64)
+    q_start, kv = i32([0, 300]), i32([4000])
+    ref, bound = attention_ref(cache, q, [0, 300], [4000], table, 128 ** -0.5, 0, KB, VB)
+    torch.cuda.synchronize()
+    need = logq.logq_kv_attention_workspace_bytes(32, 8, 128)
+    for _ in range(3):
+        dirty = torch.full((need,), 255, dtype=torch.uint8, device="cuda")         # what the allocator has at hand
+        del dirty
+        out = logq.logq_kv_attention(cache, q, q_start, kv, table, max_q=300, stream=side)
+        other = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+        side.synchronize()
+        check_attention(out, ref, bound)
+        del other
