@@ -540,8 +540,10 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         if (more) load_q(c_next);
         while (more) {
             c = c_next;
-            // the keys that this lane's four rows (16 h + 8 b + g) see: [klo, klo + seen); those
-            // that all rows of the tile see need no mask
+            // The keys that this lane's four rows (16 h + 8 b + g) see: [klo, khi).  A key tile
+            // that all rows of the warp see needs no mask, one that none of them sees no
+            // softmax: its W is zero.  (The warp's own rows decide, not the row tile's: eight
+            // prompts of 16 heads and a window of 256 53 -> 46 us.)
             int klo[4], khi[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -549,14 +551,43 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 khi[i] = pos + 1 < c.hi ? pos + 1 : c.hi;
                 klo[i] = p.window > 0 && pos >= p.window ? pos - (int)p.window + 1 : 0;
             }
-            const int tile_first = c.kv - c.n + (c.row0 + t * 128) / p.group;
-            const int tile_last = c.kv - c.n + (c.row0 + t * 128 + 127) / p.group;
-            const int all_hi = tile_first + 1, all_lo = p.window > 0 && tile_last >= p.window ? tile_last - (int)p.window + 1 : 0;
+            const int first = c.kv - c.n + (c.row0 + t * 128 + (warp & 3) * 32) / p.group;
+            const int last = c.kv - c.n + (c.row0 + t * 128 + (warp & 3) * 32 + 31) / p.group;
+            const int all_hi = first + 1, all_lo = p.window > 0 && last >= p.window ? last - (int)p.window + 1 : 0;
+            // tiles [j_lo, j_hi) hold keys that some row of the warp sees
+            const int any_lo = p.window > 0 && first >= p.window ? first - (int)p.window + 1 : 0;
+            const int j_lo = min(max(any_lo / kN - c.lo_tile, c.j0), c.j1);
+            const int j_hi = min(max(last / kN + 1 - c.lo_tile, j_lo), c.j1);
+            auto hidden_tiles = [&](int n) {
+                for (; n > 0; --n) {
+                    if (!warp_poll(sfull(t), n_s & 1u, p.ws, kWaitSoftmax)) return false;
+                    ++n_s;
+                    tc_fence_after();
+                    if (lane == 0) mbar_arrive(sempty(t));
+                    if (!warp_poll(wempty(t), n_s & 1u, p.ws, kWaitSoftmax)) return false;
+                    tc_fence_after();
+                    uint32_t w[kN / 4];
+#pragma unroll
+                    for (int i = 0; i < kN / 4; ++i) w[i] = 0;
+                    tmem_st_pairs_frag(tw, w);
+                    tmem_st_pairs_frag(tw + (16u << 16), w);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(wfull(t));
+                        mbar_arrive(rempty(slot));
+                    }
+                    if (++slot == kSlots) slot = 0;
+                }
+                return true;
+            };
             float ref[4];
             float2 sum[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) { ref[i] = kRefInit; sum[i] = make_float2(0.0f, 0.0f); }
-            for (int j = c.j0; j < c.j1; ++j) {
+            ok = hidden_tiles(j_lo - c.j0);
+            for (int j = j_lo; j < j_hi && ok; ++j) {
                 const int kb = (c.lo_tile + j) * kN;
                 ok = warp_poll(sfull(t), n_s & 1u, p.ws, kWaitSoftmax);
                 if (!ok) break;
@@ -671,7 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 }
                 if (++slot == kSlots) slot = 0;
             }
-            if (!ok) break;
+            if (!ok || !hidden_tiles(c.j1 - j_hi)) break;
             // the piece's last S is read, so Q may be replaced and the next piece begin
             more = read_piece(rd, c_next);
             if (more) load_q(c_next);
