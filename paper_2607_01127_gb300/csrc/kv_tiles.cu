@@ -237,45 +237,71 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---------------- this CTA's piece of the line ----------------
-    // A warp takes 32 requests, then sums each one's blocks with all lanes.
-    auto request_weight = [&](int64_t base) -> int64_t {
+    // kThreads requests at a time: their lengths go to shared memory (where the stages
+    // will be), then the warps in turn sum one request's blocks with all lanes.
+    int4* lens = reinterpret_cast<int4*>(smem + kStageK0);
+    int64_t* weights = reinterpret_cast<int64_t*>(smem + kStageK0 + kThreads * sizeof(int4));
+    uint32_t* weighty = reinterpret_cast<uint32_t*>(smem + kStageK0 + kThreads * (sizeof(int4) + 8));
+    static_assert(kThreads * (sizeof(int4) + 8) + 4 * (kThreads / 32) <= kStagesK * kStageBytes, "in the stages");
+    auto weigh = [&](int64_t base) -> int64_t {
         const int64_t r = base + tid;
-        Request q;
-        q.n = 0;
-        int blocks = 0;
+        int4 x = make_int4(0, 0, 0, 0);
         if (r < p.requests) {
-            q = load_request(p, r);
-            blocks = blocks_of(p, q);
+            const Request q = load_request(p, r);
+            x = make_int4(q.n, (int)q.kv, (int)q.hi, blocks_of(p, q));
         }
-        int64_t weight = 0;
-        for (uint32_t todo = __ballot_sync(0xffffffffu, blocks > 0); todo; todo &= todo - 1) {
-            const int src = __ffs(todo) - 1;
-            Request x;
-            x.q0 = 0;
-            x.n = __shfl_sync(0xffffffffu, q.n, src);
-            x.kv = __shfl_sync(0xffffffffu, q.kv, src);
-            x.hi = __shfl_sync(0xffffffffu, q.hi, src);
-            const int nb = __shfl_sync(0xffffffffu, blocks, src);
-            int64_t sum = 0;
-            for (int b = lane; b < nb; b += 32) {
-                int lo, n;
-                block_tiles(p, x, b, &lo, &n);
-                sum += n + kPieceCost;
+        const uint32_t some = __ballot_sync(0xffffffffu, x.w > 0);
+        lens[tid] = x;
+        weights[tid] = 0;
+        if (lane == 0) weighty[warp] = some;
+        __syncthreads();
+        int turn = 0;
+        for (int g = 0; g < kThreads / 32; ++g)
+            for (uint32_t todo = weighty[g]; todo; todo &= todo - 1, ++turn) {
+                if (turn % (kThreads / 32) != warp) continue;
+                const int src = g * 32 + __ffs(todo) - 1;
+                const int4 y = lens[src];
+                Request q;
+                q.q0 = 0;
+                q.n = y.x;
+                q.kv = y.y;
+                q.hi = y.z;
+                int64_t sum = 0;
+                for (int b = lane; b < y.w; b += 32) {
+                    int lo, n;
+                    block_tiles(p, q, b, &lo, &n);
+                    sum += n + kPieceCost;
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (lane == 0) weights[src] = sum * p.heads;
             }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if (lane == src) weight = sum * p.heads;
-        }
-        return weight;
+        __syncthreads();
+        return weights[tid];
     };
-    int64_t total = 0;
-    for (int64_t base = 0; base < p.requests; base += kThreads) total += request_weight(base);
+    // the requests' weights up to this thread's, and all of the batch's
+    auto scan = [&](int64_t w, int64_t* all) -> int64_t {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    if (lane == 0) sched[warp] = total;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < kThreads / 32; ++w) total += sched[w];
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t u = __shfl_up_sync(0xffffffffu, w, o);
+            if (lane >= o) w += u;
+        }
+        if (lane == 31) sched[warp] = w;
+        __syncthreads();
+        *all = 0;
+        for (int x = 0; x < kThreads / 32; ++x) {
+            const int64_t v = sched[x];
+            if (x < warp) w += v;
+            *all += v;
+        }
+        return w;
+    };
+    int64_t weight = weigh(0), batch, upto = scan(weight, &batch), total = batch;
+    for (int64_t base = kThreads; base < p.requests; base += kThreads) {
+        int64_t more;
+        scan(weigh(base), &more);
+        total += more;
+    }
     int64_t chunk = (total + gridDim.x - 1) / gridDim.x;
     chunk = chunk < kMinTiles ? kMinTiles : chunk;
     const int64_t f0 = (int64_t)blockIdx.x * chunk, f_end = f0 + chunk < total ? f0 + chunk : total;
@@ -284,29 +310,17 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         return;
     }
     int64_t before = 0;
-    for (int64_t base = 0; base < p.requests; base += kThreads) {
-        const int64_t w = request_weight(base);
-        int64_t incl = w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += u;
-        }
-        __syncthreads();
-        if (lane == 31) sched[warp] = incl;
-        __syncthreads();
-        int64_t all = 0;
-        for (int x = 0; x < kThreads / 32; ++x) {
-            if (x < warp) incl += sched[x];
-            all += sched[x];
-        }
-        const int64_t from = before + incl - w;
-        if (w > 0 && from <= f0 && f0 < from + w) {
+    for (int64_t base = 0;;) {
+        const int64_t from = before + upto - weight;
+        if (weight > 0 && from <= f0 && f0 < from + weight) {
             sched[20] = base + tid;
             sched[21] = from;
         }
-        before += all;
+        before += batch;
+        base += kThreads;
         if (f0 < before) break;                      // the same for every thread
+        weight = weigh(base);
+        upto = scan(weight, &batch);
     }
     __syncthreads();
     if (warp == kMmaWarp) {
