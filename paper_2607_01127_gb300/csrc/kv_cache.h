@@ -61,7 +61,7 @@ struct KvAttendParams {
     const int32_t* block_table;
     int64_t table_width;
     float scale_log2;        // scale * log2(e): the softmax runs in base 2
-    int32_t pad_;
+    int32_t alone;           // the tensor-memory kernel runs without the small one before it
     int64_t window;          // 0: none
     int64_t tile_rows;       // requests with more query rows (tokens x group) than this run on the tensor-memory kernel
     uint16_t* out;

@@ -233,7 +233,9 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
     // This launch follows the small kernel's of the same call and shares nothing with
     // it.  It may start when all of that one's CTAs have seen everything before the
     // call complete (they signal after their own wait), so it does not wait here but
-    // at its end: what comes next waits for this launch, and so for both.
+    // at its end: what comes next waits for this launch, and so for both.  Alone it
+    // waits here.
+    if (p.alone) asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---------------- this CTA's piece of the line ----------------

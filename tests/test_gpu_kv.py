@@ -418,3 +418,30 @@ def test_stream_argument_orders_a_calls_own_tensors():
         side.synchronize()
         check_attention(out, ref, bound)
         del other
+
+
+@pytest.mark.parametrize("hq,heads", [(8, 2), (2, 2)])
+@pytest.mark.parametrize("window", [1, 63, 64, 200])
+def test_attention_windows_narrower_than_a_tile_of_rows(window, hq, heads):
+    """Some warps of a row tile see none of a key tile that others see, before and after their own."""
+    logq = lib()
+    q_lens, kv_lens = [700, 300], [700, 1111]
+    cache, gen = filled(logq, sum(up(m, 16) for m in kv_lens), 16, heads, 64, BF, 21)
+    check_attention(*attend(logq, cache, gen, q_lens, kv_lens, hq, window=window))
+
+
+@pytest.mark.parametrize("lens", [[40, 0, 3], [1, 1, 200], [0, 0, 0], [200, 200, 200]])
+def test_attention_lengths_below_equal_bounds(lens):
+    """max_q * requests = tokens leaves no room for unequal lengths, but the device's may be shorter."""
+    logq = lib()
+    tokens, kv = 600, [500, 64, 333]
+    cache, gen = filled(logq, 64, 16, 2, 128, BF, 23)
+    q = torch.randn(tokens, 8, 128, generator=gen, device="cuda").to(BF)
+    table = torch.arange(96, dtype=torch.int32, device="cuda").view(3, 32) % 64
+    starts = [0, lens[0], lens[0] + lens[1], sum(lens)]
+    out = torch.full_like(q, 5.0)
+    logq.logq_kv_attention(cache, q, i32(starts), i32(kv), table, max_q=200, out=out)
+    if sum(lens):
+        ref = attention_ref(cache, q, starts, kv, table, 128 ** -0.5, 0, KB, VB)
+        check_attention(out[:sum(lens)], *[x[:sum(lens)] for x in ref])
+    assert (out[sum(lens):] == 5.0).all()
