@@ -509,7 +509,6 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         // ---------------- softmax, 32 query rows a warp ----------------
         const int t = warp >> 2;                     // row tile
-        const int row_in = t * 128 + (warp & 3) * 32 + lane;
         const uint32_t tq = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t ts = tq + kColS + kN * t, tw = tq + kColW + (kN / 2) * t, to = tq + kColO + 128 * t;
         int slot = 0;
@@ -720,6 +719,13 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
             }
             if (!ok || !hidden_tiles(c.j1 - j_hi)) break;
             // the piece's last S is read, so Q may be replaced and the next piece begin
+            // This lane's four rows of the result (found while the last products are still due).
+            int out_row[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = c.row0 + t * 128 + (warp & 3) * 32 + 8 * i + (lane >> 2);
+                out_row[i] = row < c.n * p.group ? (c.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group + row % p.group : -1;
+            }
             more = read_piece(rd, c_next);
             if (more) load_q(c_next);
             if (!warp_poll(wempty(t), (n_s & 1u) ^ 1u, p.ws, kWaitSoftmax)) break;
@@ -733,51 +739,54 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 l += __shfl_xor_sync(0xffffffffu, l, 1);
                 row_sum[i] = l + __shfl_xor_sync(0xffffffffu, l, 2);
             }
-            // a lane's fragments of a row are 16 contiguous bytes of 16-bit results per 32 dimensions
+            // Fragments of 64 columns (h / 2) and the lower or the upper 16 rows (h % 2): a row's
+            // 16-bit results in a lane are 16 contiguous bytes per 32 dimensions.
+            auto write_rows = [&](int h, const float* o, float f0, float f1) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int row = h & 1 ? out_row[2 + b] : out_row[b];
+                    if (row < 0) continue;
+                    const float f = b ? f1 : f0;
+                    uint16_t* dst = p.out + (int64_t)row * D + 64 * (h >> 1) + 8 * (lane & 3);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float* x = o + 16 * i + 2 * b;
+                        *reinterpret_cast<uint4*>(dst + 32 * i) =
+                            make_uint4(pack2<F16>(x[0] * f, x[1] * f), pack2<F16>(x[4] * f, x[5] * f),
+                                       pack2<F16>(x[8] * f, x[9] * f), pack2<F16>(x[12] * f, x[13] * f));
+                    }
+                }
+            };
+            // A part is kept as the fragments are, so that a warp's stores and loads are whole
+            // lines (8 prompts of 1000 tokens 118 us with rows of D and 112 so, one of 1000 34
+            // and 30).  (A warp whose rows do not exist keeps and joins nothing.)
+            const bool keeps = !whole && c.row0 + warp * 32 < c.n * p.group;
+            auto frags_of = [&](float* x, int h) { return reinterpret_cast<float4*>(x) + (warp * (D / 32) + h) * 256 + lane; };
 #pragma unroll 1
-            for (int h = 0; h < D / 32; ++h) {           // 64 columns of the lower, then of the upper 16 rows
+            for (int h = 0; h < D / 32; ++h) {
                 float o[32];
                 tmem_ld_frag(to + 64 * (h >> 1) + ((uint32_t)((h & 1) * 16) << 16), o);
                 tmem_wait_frag(o);
+                if (whole) {
+                    const float l0 = h & 1 ? row_sum[2] : row_sum[0], l1 = h & 1 ? row_sum[3] : row_sum[1];
+                    const float f0 = l0 == 0.0f ? 0.0f : 1.0f / l0, f1 = l1 == 0.0f ? 0.0f : 1.0f / l1;
+                    write_rows(h, o, f0, f1);
+                } else if (keeps) {
+                    float4* keep = frags_of(part, h);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int m = t * 128 + (warp & 3) * 32 + 16 * (h & 1) + 8 * b + (lane >> 2);
-                    const int row = c.row0 + m;
-                    const float l = h & 1 ? row_sum[2 + b] : row_sum[b];
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                    uint16_t* dst = p.out + ((int64_t)(c.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group +
-                                             row % p.group) * D + 64 * (h >> 1) + 8 * (lane & 3);
-                    float* keep = part + (size_t)m * D + 64 * (h >> 1) + 8 * (lane & 3);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float y[8];
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            y[2 * w] = o[4 * (4 * i + w) + 2 * b];
-                            y[2 * w + 1] = o[4 * (4 * i + w) + 2 * b + 1];
-                        }
-                        if (row >= c.n * p.group) continue;
-                        if (!whole) {
-                            __stcg(reinterpret_cast<float4*>(keep + 32 * i), make_float4(y[0], y[1], y[2], y[3]));
-                            __stcg(reinterpret_cast<float4*>(keep + 32 * i) + 1, make_float4(y[4], y[5], y[6], y[7]));
-                        } else {
-                            *reinterpret_cast<uint4*>(dst + 32 * i) =
-                                make_uint4(pack2<F16>(y[0] * inv, y[1] * inv), pack2<F16>(y[2] * inv, y[3] * inv),
-                                           pack2<F16>(y[4] * inv, y[5] * inv), pack2<F16>(y[6] * inv, y[7] * inv));
-                        }
-                    }
+                    for (int q = 0; q < 8; ++q) __stcg(keep + 32 * q, make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]));
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(oempty(t));
-            // (a warp whose rows do not exist has written nothing that matters and joins nothing)
-            if (!whole && c.row0 + t * 128 + (warp & 3) * 32 < c.n * p.group) {
+            if (keeps) {
+                auto stat_of = [&](float* x, int i) {
+                    return reinterpret_cast<float2*>(x + (size_t)kTileRows * D) + t * 128 + (warp & 3) * 32 + 8 * i + (lane >> 2);
+                };
                 if ((lane & 3) == 0)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        __stcg(reinterpret_cast<float2*>(part + (size_t)kTileRows * D) + t * 128 + (warp & 3) * 32 + 8 * i + (lane >> 2),
-                               make_float2(ref[i], row_sum[i]));
+                    for (int i = 0; i < 4; ++i) __stcg(stat_of(part, i), make_float2(ref[i], row_sum[i]));
                 const int c0 = c.cta0, c1 = c.cta1;
                 __threadfence();
                 __syncwarp();
@@ -786,53 +795,55 @@ __global__ void __launch_bounds__(kThreads, 1) tiles_kernel(const __grid_constan
                 if (__shfl_sync(0xffffffffu, last, 0)) {
                     __threadfence();
                     auto part_of = [&](int x) { return p.parts + (size_t)(2 * x + (x == c0 ? 1 : 0)) * tile_slot_floats(D); };
-                    auto stat_of = [&](int x) { return __ldcg(reinterpret_cast<const float2*>(part_of(x) + (size_t)kTileRows * D) + row_in); };
-                    float m = kRefInit, l = 0.0f;
-                    for (int x = c0; x <= c1; ++x) m = fmaxf(m, stat_of(x).x);
-                    for (int x = c0; x <= c1; ++x) {
-                        const float2 st = stat_of(x);
-                        l += st.y * exp2_approx(st.x - m);
-                    }
-                    const float li = l == 0.0f ? 0.0f : 1.0f / l;
-                    // a row's dimensions across the lanes, so that the parts are read in whole lines
-                    constexpr int kLanes = D / 4, kPer = 32 / kLanes;
-                    const int row = c.row0 + row_in;
-                    const int64_t off = row >= c.n * p.group ? -1 :
-                        ((int64_t)(c.q0 + row / p.group) * (p.heads * p.group) + c.head * p.group + row % p.group) * D;
-                    const int d = (lane % kLanes) * 4;
-#pragma unroll 1
-                    for (int i0 = 0; i0 < 32; i0 += 8 * kPer) {
-                        float4 y[8];
+                    float m[4], li[4];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) y[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        for (int x0 = c0; x0 <= c1; x0 += 2) {       // two parts' loads on their way at a time
-                            float k[2];
+                    for (int i = 0; i < 4; ++i) { m[i] = kRefInit; li[i] = 0.0f; }
+#pragma unroll 2
+                    for (int x = c0; x <= c1; ++x)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) m[i] = fmaxf(m[i], __ldcg(stat_of(part_of(x), i)).x);
+#pragma unroll 2
+                    for (int x = c0; x <= c1; ++x)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float2 st = __ldcg(stat_of(part_of(x), i));
+                            li[i] += st.y * exp2_approx(st.x - m[i]);
+                        }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) li[i] = li[i] == 0.0f ? 0.0f : 1.0f / li[i];
+                    // the parts' fragments in turn, two parts' loads on their way at a time
+#pragma unroll 1
+                    for (int h = 0; h < D / 32; ++h) {
+                        float y[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) y[i] = 0.0f;
+#pragma unroll 1
+                        for (int x0 = c0; x0 <= c1; x0 += 2) {
                             float4 a[2][8];
+                            float ra[2][2];
 #pragma unroll
                             for (int z = 0; z < 2; ++z) {
-                                const int x = x0 + z <= c1 ? x0 + z : c1;
-                                const float* src = part_of(x) + (size_t)(row_in - lane + i0 + lane / kLanes) * D + d;
-                                k[z] = stat_of(x).x;
+                                float* src = part_of(x0 + z <= c1 ? x0 + z : c1);
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) a[z][i] = __ldcg(reinterpret_cast<const float4*>(src + i * kPer * D));
+                                for (int q = 0; q < 8; ++q) a[z][q] = __ldcg(frags_of(src, h) + 32 * q);
+#pragma unroll
+                                for (int b = 0; b < 2; ++b) ra[z][b] = __ldcg(stat_of(src, 2 * (h & 1) + b)).x;
                             }
 #pragma unroll
                             for (int z = 0; z < 2; ++z) {
                                 if (x0 + z > c1) break;
-                                const float kz = exp2_approx(k[z] - m) * li;
+                                const float f0 = exp2_approx(ra[z][0] - (h & 1 ? m[2] : m[0])) * (h & 1 ? li[2] : li[0]);
+                                const float f1 = exp2_approx(ra[z][1] - (h & 1 ? m[3] : m[1])) * (h & 1 ? li[3] : li[1]);
 #pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    const float f = __shfl_sync(0xffffffffu, kz, i0 + i * kPer + lane / kLanes);
-                                    y[i].x += a[z][i].x * f; y[i].y += a[z][i].y * f; y[i].z += a[z][i].z * f; y[i].w += a[z][i].w * f;
+                                for (int q = 0; q < 8; ++q) {
+                                    y[4 * q] += a[z][q].x * f0;
+                                    y[4 * q + 1] += a[z][q].y * f0;
+                                    y[4 * q + 2] += a[z][q].z * f1;
+                                    y[4 * q + 3] += a[z][q].w * f1;
                                 }
                             }
                         }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int64_t o = __shfl_sync(0xffffffffu, off, i0 + i * kPer + lane / kLanes);
-                            if (o >= 0)
-                                *reinterpret_cast<uint2*>(p.out + o + d) = make_uint2(pack2<F16>(y[i].x, y[i].y), pack2<F16>(y[i].z, y[i].w));
-                        }
+                        write_rows(h, y, 1.0f, 1.0f);
                     }
                 }
             }
