@@ -67,6 +67,8 @@ __device__ __forceinline__ float scaled_range(float r)
 // How a segment [line, line + places) is shared by CTAs whose raw pieces are
 // `chunk` places each.  A cut next to either end moves there, and every cut of a
 // short segment does, because parts cost a join (they go through global memory).
+// margin (how near is near) is at most half of `places`: a start moved beyond the
+// segment's end would be nobody's.
 struct Sharing {
     int first, last;         // CTAs: the segment is one CTA's where they are equal
 };

@@ -72,11 +72,13 @@ logq_status status_of(cudaError_t e)
 // Requests with at most kTileMinRows query rows (tokens x query heads per kv head)
 // run on the small kernel, which re-reads the keys for every 24 of them; the tiles
 // of the large one hold 256.  Measured with 8 kv heads x 128: 16 requests of 48 rows
-// and 2000 keys 39 us on the small and 66 us on the large kernel, of 96 rows 67 and
-// 66, of 160 rows 108 and 66; 64 requests of 48 rows and 500 keys 53 and 74, of 96
-// rows 103 and 74.  A call of at most kTileMinTotal rows in all does not fill the
-// large kernel's tiles: one request of 96 rows and 4000 keys takes 19 and 55 us.
-constexpr int64_t kTileMinRows = 64, kTileMinTotal = 128;
+// and 2000 keys 39 us on the small and 48 us on the large kernel, of 96 rows 68 and
+// 49, of 160 rows 108 and 50; 64 requests of 48 rows and 500 keys 54 and 57, of 96
+// rows 103 and 58.  A call of at most kTileMinTotal rows in all does not fill the
+// large kernel's SMs: one request of 256 rows and 1000 keys takes 17 and 27 us, of
+// 4000 keys 30 and 47, of 16000 keys 70 and 65; of 384 rows 20 and 27, 35 and 40,
+// 96 and 63.
+constexpr int64_t kTileMinRows = 64, kTileMinTotal = 256;
 
 int sms_or_default() { return sm_count() > 0 ? sm_count() : 148; }
 
