@@ -14,13 +14,15 @@
 // as fragments of four rows x 16 keys, so that a key's three range values are loaded
 // once for four rows (a row per lane took 40% of shared memory's cycles for them).
 //
-// What bounds it: a key tile costs 1152 cycles of MMA at D = 128 and shared memory
-// about as much (operands, decoded values written, pair-table lookups, ranges), a
-// row tile's softmax somewhat more, so the two row tiles run independently and S of
-// the next key tile is computed while the softmax works on this one: W has a place
-// of its own.  That takes 64 columns more than tensor memory has, so half of Q (at
-// D = 128) is an operand in shared memory, whose re-reads slow those products by
-// half (48 cycles instead of 32).
+// What bounds it: a key tile costs 1152 cycles of MMA at D = 128, a row tile's softmax
+// somewhat more, so the two row tiles run independently and S of the next key tile is
+// computed while the softmax works on this one: W has a place of its own.  That takes
+// 64 columns more than tensor memory has, so half of Q (at D = 128) is an operand in
+// shared memory, whose re-reads slow those products by half (48 cycles instead of 32).
+// Shared memory then takes more than the MMAs: by the counters a key tile moves ~2400
+// wavefronts through the SM's data pipe (the products' operands 734, look-ups 256 and
+// about as many replays, ranges 384, decoded values 290, the rest tensor-memory stores
+// and global loads) in ~2500 cycles.
 //
 // Tensor memory: S0 S1 (64 columns each) | W0 W1 (32) | Q0 Q1 (32: dimensions 0 .. 63)
 // | O0 O1 (128).
@@ -31,12 +33,13 @@
 // Split: as in the small kernel the segments' key tiles form one line that the
 // CTAs cut evenly; the last warp to arrive joins the parts of its 32 rows.
 //
-// Measured: one 8192-token prompt of 32 query and 8 kv heads x 128 in 556 us, 989
+// Measured: one 8192-token prompt of 32 query and 8 kv heads x 128 in 552 us, 996
 // TFLOP/s of the visible products (0.50 of the measured bf16 rate); a key tile takes
-// 2340 cycles.  Tensor pipe 36 % active (both row tiles' unmasked halves counted by
-// what they cost), shared-memory pipe 59 %: no single role or pipe binds.  400 extra
-// cycles in any one role change nothing, while more shared-memory traffic or more
-// integer work (decoding by byte permutes instead of look-ups: 595 us) slow it.
+// about 2300 cycles.  Without the loads of the ranges (and so wrong) it takes 6 % less,
+// without the look-ups 3 %; half the exponentials change nothing, and neither do 400
+// extra cycles in any one role, while more integer work slows it (decoding by byte
+// permutes instead of look-ups: 595 us; keys' ranges kept in 16 bits and the values'
+// inverses computed: 3 % slower).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <stdint.h>
